@@ -70,7 +70,9 @@ typedef enum {
   OMNI_CALL_BLOCK_SCORES = 10,
   OMNI_CALL_PREFILL_SELECT = 11,
   OMNI_CALL_BLOCK_ATTN_FWD = 12,
-  OMNI_CALL_BLOCK_ATTN_BWD = 13
+  OMNI_CALL_BLOCK_ATTN_BWD = 13,
+  OMNI_CALL_PAGED_ATTN = 14,
+  OMNI_CALL_PAGED_EVICT = 15
 } omni_call_id;
 
 /* One attention layer during prefill / training.
@@ -118,6 +120,31 @@ typedef struct {
   int32_t page_rows;           /* rows per page, a power of two */
   int32_t pages_cap;           /* table entries per pair; pages_cap * page_rows >= u_cap of the call */
 } omni_page_pool;
+
+/* Rotary positions: the pairs of the first rot_dim elements of a head are turned by
+ * position * inv_freq, the rest is copied.  Fill inv_freq with omni_rope_frequencies
+ * (or with frequencies of your own). */
+typedef struct {
+  int32_t head_dim;            /* 64 or 128 */
+  int32_t rot_dim;             /* a multiple of 16, at most head_dim */
+  int32_t interleaved;         /* 1: pair i is elements (2i, 2i + 1); 0: (i, i + rot_dim / 2) */
+  float out_scale;             /* magnitude given to the rotated pairs (1: a pure rotation) */
+  double inv_freq[64];         /* angle per position of pair i < rot_dim / 2, radians */
+} omni_rope_desc;
+
+/* A chunk of new tokens of every sequence in front of its paged cache (omni_paged_append,
+ * omni_paged_attn, omni_paged_evict).  The sequences of a padded batch have their own
+ * numbers of new tokens, device arrays new_cnt [batch]; values outside [0, n_new] count as
+ * the nearest of these. */
+typedef struct {
+  int32_t batch, n_q_heads, n_kv_heads, head_dim;
+  int32_t n_new;               /* padded length of the chunk */
+  int32_t causal;              /* 1: a new token sees the rows up to its own; 0: every row */
+  int32_t dtype;               /* omni_dtype of Q, K, V, O and of the pool */
+  float softmax_scale;
+  int64_t q_stride[3];         /* batch, head, token strides of Q and of what is shaped like it, in elements */
+  int64_t kv_stride[3];        /* same for the chunk's K and V */
+} omni_chunk_desc;
 
 /*
  * omni_score_queries -- Sec. "Query Selection as Binary Lazy-Active
@@ -592,11 +619,117 @@ int omni_dense_decode(const omni_decode_desc* desc, const void* q,
                       const void* Kcache, const void* Vcache, const int32_t* ctx_len,
                       void* O, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * Rotary positions.  With the angle a = position * inv_freq[i] a pair (u, v) becomes
+ *   (u cos a - v sin a, u sin a + v cos a) * out_scale.
+ * Angles are formed and reduced in 64 bits (a position of a million turns the fastest
+ * pair 1.6e5 times: 32 bits would leave three digits of the angle), the pairs are turned
+ * in 32 bits and rounded once.
+ *
+ * omni_rope_frequencies fills rope->inv_freq on the host (a plan: once per model; the
+ * other fields must be set): f_i = base^(-2 i / rot_dim), and by `scaling`
+ *   0 (none)      f_i
+ *   1 (linear)    f_i / factor: positions are stretched
+ *   2 (by parts)  f_i (s + (1 - s) / factor) with s = (turns - low_turns) / (high_turns -
+ *                 low_turns) cut to [0, 1] and turns = orig_len f_i / (2 pi): pairs that turn
+ *                 often inside the original length keep their frequency, those that turn
+ *                 rarely are stretched, the others lie in between.
+ *   base > 1; factor > 0 (1 and 2); orig_len > 0 and low_turns < high_turns (2)
+ *
+ * omni_rope turns Q and K of a layer in one launch, as needed before the attention calls
+ * (backward = 0), or applies the transposed map to the gradients dQ and dK that
+ * omni_sparse_attn_bwd returns (backward = 1: the angles negated, the same out_scale).
+ *   desc  batch, heads, head_dim, n_tokens, dtype and strides are used
+ *   pos   [batch, n_tokens] i32, any sign; null: token n is at position n
+ *   Qout, Kout: same shapes and strides as Q and K; may be Q and K themselves
+ */
+int omni_rope_frequencies(omni_rope_desc* rope /* host */, double base, int scaling, double factor,
+                          double orig_len, double low_turns, double high_turns);
+int omni_rope(const omni_rope_desc* rope, const omni_layer_desc* desc, const void* Q, const void* K,
+              const int32_t* pos, int backward, void* Qout, void* Kout, void* stream);
+
+/*
+ * A cache that grows and shrinks in pages (omni_page_pool; here a table entry holds rows
+ * [e * page_rows, (e + 1) * page_rows) of its (sequence, KV head) pair, and a pair can hold
+ * rows_cap = pages_cap * page_rows rows).  Every row carries its token's position and,
+ * where the caller wants to evict by it, the attention weight it has collected:
+ *   row_pos [batch, n_kv_heads, rows_cap] i32, acc [batch, n_kv_heads, rows_cap] f32.
+ * One step of a serving loop is
+ *   omni_paged_append   new rows behind the old ones  (row_cnt -> row_end)
+ *   omni_paged_attn     attention of the new tokens   (row_end)
+ *   omni_paged_evict    back to the budget            (row_end -> row_cnt)
+ * each reading its counts from device memory: the three can be captured in one HIP graph
+ * that is replayed per token.  The pages of the rows in use have to be in the table and
+ * must not be shared where rows are written; table entries outside [0, n_pages) are
+ * pages that are not there: nothing is stored in their rows and nobody attends them.
+ * Counts below 0 or above rows_cap count as the nearest of these.  Rows behind the last
+ * one in use are neither read nor written.
+ *
+ * omni_paged_append -- new token t < new_cnt[b] of sequence b, at position pos[b] + t, is
+ * stored as row row_cnt[b, g] + t of every KV head g: K turned by rope (null: as it is), V,
+ * row_pos, and acc = 0 (acc may be null).  row_end[b, g] = row_cnt[b, g] + new_cnt[b]
+ * (rows_cap at most; rows that do not fit are dropped).  With rope, Q is turned too:
+ *   Q [batch, n_q_heads, n_new, head_dim] -> Qout, same strides, may be Q itself; rows
+ *   t >= new_cnt[b] are not written.  Without rope both must be null.
+ *   K, V [batch, n_kv_heads, n_new, head_dim]; pos, new_cnt [batch] i32
+ *   row_cnt, row_end [batch, n_kv_heads] i32, two different arrays
+ */
+int omni_paged_append(const omni_chunk_desc* desc, const omni_rope_desc* rope, const void* Q,
+                      const void* K, const void* V, const omni_page_pool* pool,
+                      const int32_t* pos, const int32_t* new_cnt, const int32_t* row_cnt,
+                      void* Qout, int32_t* row_end, int32_t* row_pos, float* acc, void* stream);
+
+/*
+ * omni_paged_attn -- attention of a chunk of new tokens over the pages, one token to many.
+ * The chunk's own rows are the last new_cnt[b] of the row_end[b, g] rows of a pair, so new
+ * token t sees rows [0, row_end - new_cnt + t] (causal) or all of them:
+ *   O = softmax(q . K^T softmax_scale) V,  lse = log sum exp of the scaled products.
+ * A token that sees no row, and t >= new_cnt[b], get O = 0 and lse = -inf.  Q of the
+ * latter and rows nobody sees are not read for values: they may hold anything.  V of a
+ * stored row that only some tokens of the chunk see has to be finite.
+ * With acc_out the weights of the step are added per row (the sum over the query heads of
+ * the KV head and over the new tokens of the attention probabilities):
+ *   acc_out[b, g, j] = acc_in[b, g, j] + sum p[j]     for j < row_end[b, g]
+ * acc_in null counts as zeros; acc_in may be acc_out; both null: no weights.
+ *   Q [batch, n_q_heads, n_new, head_dim], O the same shape and strides
+ *   lse [batch, n_q_heads, n_new] f32, out
+ *   page_rows at least 16
+ * bf16: both products on the bf16 matrix cores (the probabilities rounded to bf16 for the
+ * second), sums in fp32; fp32: fp32 matrix cores.
+ * Workspace: OMNI_CALL_PAGED_ATTN with param = rows_cap where acc_out is given, else 0.
+ */
+int omni_paged_attn(const omni_chunk_desc* desc, const void* Q, const omni_page_pool* pool,
+                    const int32_t* row_end, const int32_t* new_cnt, void* O, float* lse,
+                    const float* acc_in, float* acc_out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * omni_paged_evict -- per pair the min(row_end, budget) rows that stay: those spared by
+ * their position (row_pos < n_sink, or row_pos >= seq_len[b] - n_recent) before all others,
+ * then those of largest acc (NaN below everything); equal ones by lowest row.  The rows
+ * that stay move together without keeping their order: of the rows that leave, those in
+ * front of the new end are holes, and the k-th hole takes the k-th staying row from
+ * behind the new end.  Only those rows are copied (K, V in the pages; the attention of
+ * later tokens does not depend on the order of the rows), and a page behind the new end is
+ * free afterwards.
+ *   desc    batch, n_kv_heads, head_dim and dtype are used
+ *   budget  rows per pair, >= 1 and >= n_sink + n_recent; n_sink, n_recent >= 0
+ *   seq_len [batch] i32: the position after the last token
+ *   row_end [batch, n_kv_heads] i32, row_pos, acc [batch, n_kv_heads, rows_cap]: in
+ *   row_cnt [batch, n_kv_heads] i32, row_pos_out, acc_out [batch, n_kv_heads, rows_cap], out:
+ *           the counts, and for rows below them what the rows carry; each may be its input
+ * Workspace: OMNI_CALL_PAGED_EVICT with param = rows_cap.
+ */
+int omni_paged_evict(const omni_chunk_desc* desc, const omni_page_pool* pool, int32_t budget,
+                     int32_t n_sink, int32_t n_recent, const int32_t* seq_len, const int32_t* row_end,
+                     const int32_t* row_pos, const float* acc, int32_t* row_cnt,
+                     int32_t* row_pos_out, float* acc_out, void* ws, size_t ws_bytes, void* stream);
+
 /* Workspace bytes needed by call `call_id` (omni_call_id) for the given
  * descriptor (omni_layer_desc* for prefill calls, omni_decode_desc* for the two
- * decode calls).  `param` is the index capacity b_cap for the calls that take
+ * decode calls, omni_chunk_desc* for the two paged ones).  `param` is the index capacity b_cap for the calls that take
  * one, the probe block for OMNI_CALL_KV_BUDGET and OMNI_CALL_PREFILL_SELECT,
- * blk_cap * block for OMNI_CALL_BLOCK_ATTN_FWD and OMNI_CALL_BLOCK_ATTN_BWD, and ignored otherwise.
+ * blk_cap * block for OMNI_CALL_BLOCK_ATTN_FWD and OMNI_CALL_BLOCK_ATTN_BWD,
+ * rows_cap (or 0) as said there for the paged calls, and ignored otherwise.
  * Returns 0 on invalid input (a valid call never needs 0 bytes). */
 size_t omni_workspace_bytes(int call_id, const void* desc, int32_t param);
 

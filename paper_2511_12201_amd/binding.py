@@ -19,7 +19,8 @@ LIB_PATH = os.path.join(_HERE, "libomnisparse.so")
 OMNI_F32, OMNI_BF16 = 0, 1
 (CALL_SCORE_QUERIES, CALL_SELECT_QUERIES, CALL_KV_BUDGET, CALL_SELECT_KV, CALL_SPARSE_ATTN_FWD,
  CALL_SPARSE_ATTN_BWD, CALL_SLIM_DECODE, CALL_DENSE_ATTN_FWD, CALL_DENSE_DECODE, CALL_GROUP_SUBSET,
- CALL_BLOCK_SCORES, CALL_PREFILL_SELECT, CALL_BLOCK_ATTN_FWD, CALL_BLOCK_ATTN_BWD) = range(14)
+ CALL_BLOCK_SCORES, CALL_PREFILL_SELECT, CALL_BLOCK_ATTN_FWD, CALL_BLOCK_ATTN_BWD, CALL_PAGED_ATTN,
+ CALL_PAGED_EVICT) = range(16)
 
 EXPORTED = [
     "omni_score_queries", "omni_select_queries", "omni_kv_budget", "omni_budget_from_scores", "omni_select_kv",
@@ -35,6 +36,7 @@ EXPORTED = [
     "omni_debug_attention_route", "omni_debug_device_work_list",
     "omni_slim_decode_grouped_static", "omni_static_scratch_bytes",
     "omni_sparse_prefill", "omni_sparse_prefill_workspace_bytes", "omni_slim_decode_prepare",
+    "omni_rope_frequencies", "omni_rope", "omni_paged_append", "omni_paged_attn", "omni_paged_evict",
 ]
 
 PROF_KERNELS = {"attn_fwd": 0, "pack_kv": 1, "clear_out": 2, "pool_q": 3, "probe_lse": 4, "probe_sum": 5,
@@ -63,6 +65,21 @@ class PagePool(C.Structure):
     _fields_ = [
         ("K", C.c_void_p), ("V", C.c_void_p), ("page_table", C.c_void_p),
         ("n_pages", C.c_int32), ("page_rows", C.c_int32), ("pages_cap", C.c_int32),
+    ]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [
+        ("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("out_scale", C.c_float),
+        ("inv_freq", C.c_double * 64),
+    ]
+
+
+class ChunkDesc(C.Structure):
+    _fields_ = [
+        ("batch", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("n_new", C.c_int32), ("causal", C.c_int32), ("dtype", C.c_int32), ("softmax_scale", C.c_float),
+        ("q_stride", C.c_int64 * 3), ("kv_stride", C.c_int64 * 3),
     ]
 
 
@@ -141,6 +158,11 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.omni_slim_decode_compact.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
     lib.omni_compact_cache_paged.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp]
     lib.omni_slim_decode_paged.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.omni_rope_frequencies.argtypes = [vp, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double, C.c_double]
+    lib.omni_rope.argtypes = [vp, vp, vp, vp, vp, C.c_int, vp, vp, vp]
+    lib.omni_paged_append.argtypes = [vp] * 14
+    lib.omni_paged_attn.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.omni_paged_evict.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.omni_profile_enable.argtypes = [C.c_int]
     lib.omni_debug_copy.argtypes = [vp, vp, sz, vp]
     lib.omni_debug_key_split_len.argtypes = [C.c_int]
@@ -212,6 +234,54 @@ def make_decode_desc(q: torch.Tensor, Kcache: torch.Tensor, vis_begin: int, vis_
     d.tau = tau
     d.kv_stride = (C.c_int64 * 3)(*Kcache.stride()[:3])
     d.static_lists = 1 if static_lists else 0
+    return d
+
+
+ROPE_SCALING = {"none": 0, "linear": 1, "by_parts": 2}
+
+
+def make_rope_desc(head_dim: int, rot_dim: int | None = None, *, base: float = 10000.0, interleaved: bool = False,
+                   scaling: str = "none", factor: float = 1.0, orig_len: float = 0.0, low_turns: float = 1.0,
+                   high_turns: float = 32.0, out_scale: float = 1.0) -> RopeDesc:
+    """Plan of omni_rope and omni_paged_append: which elements of a head form pairs, and the pairs' frequencies
+    (scaling "none", "linear" or "by_parts" as in omni_rope_frequencies).  Made once per model."""
+    if scaling not in ROPE_SCALING:
+        raise ValueError(f"scaling must be one of {sorted(ROPE_SCALING)}")
+    r = RopeDesc()
+    r.head_dim, r.rot_dim = head_dim, head_dim if rot_dim is None else rot_dim
+    r.interleaved, r.out_scale = int(interleaved), out_scale
+    _check(load_library().omni_rope_frequencies(C.byref(r), base, ROPE_SCALING[scaling], factor, orig_len, low_turns,
+                                                high_turns))
+    return r
+
+
+def _row_strides(x: torch.Tensor):
+    """Batch, head and token strides of x [B, H, n, D]; a dimension of one element takes the stride it would have in a
+    contiguous tensor, since torch may hold any number there."""
+    if x.dim() != 4 or x.stride(3) != 1:
+        raise ValueError("need [batch, heads, tokens, head_dim] with a contiguous head_dim")
+    B, H, n, D = x.shape
+    return (C.c_int64 * 3)(*(s if size > 1 else natural for s, size, natural in
+                             zip(x.stride(), (B, H, n), (H * n * D, n * D, D))))
+
+
+def make_chunk_desc(Q: torch.Tensor, K: torch.Tensor | None = None, *, n_kv_heads: int | None = None, causal: bool = True,
+                    softmax_scale: float | None = None) -> ChunkDesc:
+    """Chunk of new tokens, Q [B, Hq, n_new, D] and K [B, Hkv, n_new, D] (V has K's strides).  omni_paged_attn needs no K:
+    n_kv_heads instead."""
+    d = ChunkDesc()
+    d.batch, d.n_q_heads, d.n_new, d.head_dim = Q.shape
+    if K is None and n_kv_heads is None:
+        raise ValueError("give K or n_kv_heads")
+    if K is not None and ((K.shape[0], K.shape[2], K.shape[3]) != (Q.shape[0], Q.shape[2], Q.shape[3]) or K.dtype != Q.dtype
+                          or n_kv_heads not in (None, K.shape[1])):
+        raise ValueError("K must be [batch, n_kv_heads, n_new, head_dim] of Q's dtype")
+    d.n_kv_heads = K.shape[1] if K is not None else n_kv_heads
+    d.causal, d.dtype = int(causal), _dtype_code(Q)
+    d.softmax_scale = softmax_scale if softmax_scale is not None else Q.shape[3] ** -0.5
+    d.q_stride = _row_strides(Q)
+    natural = (d.n_kv_heads * d.n_new * d.head_dim, d.n_new * d.head_dim, d.head_dim)
+    d.kv_stride = _row_strides(K) if K is not None else (C.c_int64 * 3)(*natural)
     return d
 
 
@@ -830,3 +900,187 @@ def omni_dense_decode(desc: DecodeDesc, q, Kcache, Vcache, ctx_len, O=None, ws: 
     _check(lib.omni_dense_decode(C.byref(desc), _ptr(q), _ptr(Kcache), _ptr(Vcache), _ptr(ctx_len), _ptr(O), _ptr(buf),
                                  buf.numel(), _stream()))
     return O
+
+
+# ------------------------------------------------------------------ rotary positions and the paged cache
+#
+# These calls run on the current stream of their tensors' device.  Without a workspace of the caller's they take their
+# scratch from torch's allocator, call by call: calls on two streams, and two captured graphs, then never share any.
+
+_DTYPES = {OMNI_BF16: torch.bfloat16, OMNI_F32: torch.float32}
+
+
+def _run_on(dev: torch.device, fn, *args):
+    """fn(*args, stream) on the tensors' device and its current stream."""
+    if dev.type != "cuda":
+        raise ValueError(f"tensors must be on the GPU, not on {dev}")
+    if dev.index == torch.cuda.current_device():
+        return _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+    with torch.cuda.device(dev):
+        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+
+
+def _want(name: str, t: torch.Tensor, dtype, shape, dev):
+    """Refuse a tensor that the kernels would misread: its type, shape, device and density."""
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor {tuple(shape)} on {dev}, got {t.dtype} "
+                         f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
+
+
+def _want_rows(name: str, t: torch.Tensor, dtype, shape, strides, dev):
+    """The same for what is shaped like Q or K: the strides are the descriptor's."""
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or t.stride(3) != 1 or \
+            any(t.shape[k] > 1 and t.stride(k) != strides[k] for k in range(3)):
+        raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)} with strides {tuple(strides)} and 1 on {dev}, got "
+                         f"{t.dtype} {tuple(t.shape)} with {t.stride()} on {t.device}")
+
+
+def _like(t: torch.Tensor, strides) -> torch.Tensor:
+    """An uninitialised tensor of t's shape and type with the descriptor's strides."""
+    return torch.empty_strided(t.shape, (*strides, 1), dtype=t.dtype, device=t.device)
+
+
+def _scratch(ws: Workspace | None, call_id: int, desc, param: int, dev):
+    if ws is not None:
+        return ws.get(call_id, desc, param)
+    return torch.empty(workspace_bytes(call_id, desc, param), dtype=torch.uint8, device=dev)
+
+
+def _pool_of(pool: PagePool, dtype, head_dim: int, dev):
+    """(batch, n_kv_heads, rows_cap) of a pool whose tensors fit the call."""
+    K, V, table = pool._keep
+    if K.dtype is not dtype or V.dtype is not dtype or K.shape[-1] != head_dim:
+        raise ValueError("pool dtype / head_dim differ from the call's")
+    if K.device != dev or V.device != dev or table.device != dev:
+        raise ValueError(f"pool and page table must be on {dev}")
+    if table.dim() != 3:
+        raise ValueError("page_table must be [batch, n_kv_heads, pages_cap]")
+    return table.shape[0], table.shape[1], pool.pages_cap * pool.page_rows
+
+
+def omni_rope(rope: RopeDesc, desc: LayerDesc, Q, K, pos=None, backward: bool = False, Qout=None, Kout=None):
+    """Rotary positions of a layer's Q and K, or (backward) of the gradients dQ and dK: (Qout, Kout).  pos [B, N] int32 (None:
+    0, 1, ..); the outputs may be the inputs."""
+    dev, dt = Q.device, _DTYPES[desc.dtype]
+    qs, ks = list(desc.q_stride), list(desc.kv_stride)
+    B, N, D = desc.batch, desc.n_tokens, desc.head_dim
+    _want_rows("Q", Q, dt, (B, desc.n_q_heads, N, D), qs, dev)
+    _want_rows("K", K, dt, (B, desc.n_kv_heads, N, D), ks, dev)
+    if pos is not None:
+        _want("pos", pos, torch.int32, (B, N), dev)
+    if Qout is None:
+        Qout = _like(Q, qs)
+    elif Qout is not Q:
+        _want_rows("Qout", Qout, dt, Q.shape, qs, dev)
+    if Kout is None:
+        Kout = _like(K, ks)
+    elif Kout is not K:
+        _want_rows("Kout", Kout, dt, K.shape, ks, dev)
+    _run_on(dev, load_library().omni_rope, C.byref(rope), C.byref(desc), Q.data_ptr(), K.data_ptr(),
+            None if pos is None else pos.data_ptr(), int(backward), Qout.data_ptr(), Kout.data_ptr())
+    return Qout, Kout
+
+
+def omni_paged_append(desc: ChunkDesc, rope: RopeDesc | None, Q, K, V, pool: PagePool, pos, new_cnt, row_cnt, row_pos, acc=None,
+                      Qout=None, row_end=None):
+    """Store a chunk's K (turned) and V behind the rows of its pages and turn its Q: (Qout, row_end).  Without rope Q is None
+    and K is stored as it is.  row_pos and acc [B, Hkv, rows_cap] get the new rows' positions and zeros."""
+    dev, dt = K.device, _DTYPES[desc.dtype]
+    B, Hkv, n, D = desc.batch, desc.n_kv_heads, desc.n_new, desc.head_dim
+    ks = list(desc.kv_stride)
+    tb, th, cap = _pool_of(pool, dt, D, dev)
+    if (tb, th) != (B, Hkv):
+        raise ValueError(f"page_table is for {tb} x {th} pairs, the chunk has {B} x {Hkv}")
+    _want_rows("K", K, dt, (B, Hkv, n, D), ks, dev)
+    _want_rows("V", V, dt, (B, Hkv, n, D), ks, dev)
+    if rope is not None:
+        qs = list(desc.q_stride)
+        _want_rows("Q", Q, dt, (B, desc.n_q_heads, n, D), qs, dev)
+        if Qout is None:
+            Qout = _like(Q, qs)
+        elif Qout is not Q:
+            _want_rows("Qout", Qout, dt, Q.shape, qs, dev)
+    elif Q is not None or Qout is not None:
+        raise ValueError("Q and Qout are for calls with rope")
+    _want("pos", pos, torch.int32, (B,), dev)
+    _want("new_cnt", new_cnt, torch.int32, (B,), dev)
+    _want("row_cnt", row_cnt, torch.int32, (B, Hkv), dev)
+    _want("row_pos", row_pos, torch.int32, (B, Hkv, cap), dev)
+    if acc is not None:
+        _want("acc", acc, torch.float32, (B, Hkv, cap), dev)
+    if row_end is None:
+        row_end = torch.empty_like(row_cnt)
+    else:
+        _want("row_end", row_end, torch.int32, (B, Hkv), dev)
+    _run_on(dev, load_library().omni_paged_append, C.byref(desc), None if rope is None else C.byref(rope),
+            None if Q is None else Q.data_ptr(), K.data_ptr(), V.data_ptr(), C.byref(pool), pos.data_ptr(), new_cnt.data_ptr(),
+            row_cnt.data_ptr(), None if Qout is None else Qout.data_ptr(), row_end.data_ptr(), row_pos.data_ptr(),
+            None if acc is None else acc.data_ptr())
+    return Qout, row_end
+
+
+def omni_paged_attn(desc: ChunkDesc, Q, pool: PagePool, row_end, new_cnt, O=None, lse=None, acc_in=None, acc_out=None,
+                    ws: Workspace | None = None):
+    """Attention of a chunk of new tokens over the pages: (O, lse).  acc_out [B, Hkv, rows_cap] gets acc_in (None: zeros) plus
+    the rows' attention weights of this step; it may be acc_in."""
+    dev, dt = Q.device, _DTYPES[desc.dtype]
+    B, Hq, Hkv, n, D = desc.batch, desc.n_q_heads, desc.n_kv_heads, desc.n_new, desc.head_dim
+    qs = list(desc.q_stride)
+    tb, th, cap = _pool_of(pool, dt, D, dev)
+    if (tb, th) != (B, Hkv):
+        raise ValueError(f"page_table is for {tb} x {th} pairs, the chunk has {B} x {Hkv}")
+    _want_rows("Q", Q, dt, (B, Hq, n, D), qs, dev)
+    _want("row_end", row_end, torch.int32, (B, Hkv), dev)
+    _want("new_cnt", new_cnt, torch.int32, (B,), dev)
+    if O is None:
+        O = _like(Q, qs)
+    else:
+        _want_rows("O", O, dt, Q.shape, qs, dev)
+    if lse is None:
+        lse = torch.empty(B, Hq, n, dtype=torch.float32, device=dev)
+    else:
+        _want("lse", lse, torch.float32, (B, Hq, n), dev)
+    if acc_in is not None:
+        _want("acc_in", acc_in, torch.float32, (B, Hkv, cap), dev)
+    if acc_out is not None:
+        _want("acc_out", acc_out, torch.float32, (B, Hkv, cap), dev)
+    buf = _scratch(ws, CALL_PAGED_ATTN, desc, cap if acc_out is not None else 0, dev)
+    _run_on(dev, load_library().omni_paged_attn, C.byref(desc), Q.data_ptr(), C.byref(pool), row_end.data_ptr(),
+            new_cnt.data_ptr(), O.data_ptr(), lse.data_ptr(), None if acc_in is None else acc_in.data_ptr(),
+            None if acc_out is None else acc_out.data_ptr(), buf.data_ptr(), buf.numel())
+    return O, lse
+
+
+def omni_paged_evict(pool: PagePool, budget: int, n_sink: int, n_recent: int, seq_len, row_end, row_pos, acc, row_cnt=None,
+                     row_pos_out=None, acc_out=None, ws: Workspace | None = None):
+    """Keep the `budget` rows of every pair that collected most attention weight (and those spared by their position), the rest
+    of the pages free: (row_cnt, row_pos_out, acc_out).  Outputs that are not given are new tensors; pass row_pos and acc
+    themselves to work in place."""
+    K, _, table = pool._keep
+    dev = K.device
+    B, Hkv, cap = _pool_of(pool, K.dtype, K.shape[-1], dev)
+    _want("seq_len", seq_len, torch.int32, (B,), dev)
+    _want("row_end", row_end, torch.int32, (B, Hkv), dev)
+    _want("row_pos", row_pos, torch.int32, (B, Hkv, cap), dev)
+    _want("acc", acc, torch.float32, (B, Hkv, cap), dev)
+    if row_cnt is None:
+        row_cnt = torch.empty_like(row_end)
+    else:
+        _want("row_cnt", row_cnt, torch.int32, (B, Hkv), dev)
+    if row_pos_out is None:
+        row_pos_out = torch.empty_like(row_pos)
+    else:
+        _want("row_pos_out", row_pos_out, torch.int32, (B, Hkv, cap), dev)
+    if acc_out is None:
+        acc_out = torch.empty_like(acc)
+    else:
+        _want("acc_out", acc_out, torch.float32, (B, Hkv, cap), dev)
+    d = ChunkDesc()
+    d.batch, d.n_q_heads, d.n_kv_heads, d.head_dim, d.n_new, d.causal, d.dtype = B, Hkv, Hkv, K.shape[-1], 1, 1, _dtype_code(K)
+    d.softmax_scale = 1.0
+    d.q_stride = d.kv_stride = (C.c_int64 * 3)(Hkv * d.head_dim, d.head_dim, d.head_dim)
+    buf = _scratch(ws, CALL_PAGED_EVICT, d, cap, dev)
+    _run_on(dev, load_library().omni_paged_evict, C.byref(d), C.byref(pool), budget, n_sink, n_recent, seq_len.data_ptr(),
+            row_end.data_ptr(), row_pos.data_ptr(), acc.data_ptr(), row_cnt.data_ptr(), row_pos_out.data_ptr(),
+            acc_out.data_ptr(), buf.data_ptr(), buf.numel())
+    return row_cnt, row_pos_out, acc_out

@@ -10,6 +10,7 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "paged.h"
 #include "sched.h"
 
 namespace omni {
@@ -70,6 +71,58 @@ int validate_decode(const omni_decode_desc* d) {
       OMNI_FAIL(OMNI_ERR_INVALID, "cache strides must be multiples of 8 elements and at least head_dim");
   if (d->static_lists != 0 && d->static_lists != 1) OMNI_FAIL(OMNI_ERR_INVALID, "static_lists must be 0 or 1");
   return OMNI_OK;
+}
+
+static int validate_chunk(const omni_chunk_desc* d) {
+  if (!d) OMNI_FAIL(OMNI_ERR_INVALID, "descriptor is null");
+  if (d->batch < 1 || d->n_q_heads < 1 || d->n_kv_heads < 1 || d->n_new < 1)
+    OMNI_FAIL(OMNI_ERR_INVALID, "batch, head counts and n_new must be positive");
+  if (d->n_q_heads % d->n_kv_heads) OMNI_FAIL(OMNI_ERR_INVALID, "n_q_heads must be a multiple of n_kv_heads");
+  if (d->head_dim != 64 && d->head_dim != 128) OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  if (d->dtype != OMNI_F32 && d->dtype != OMNI_BF16) OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "dtype must be OMNI_F32 or OMNI_BF16");
+  if (d->causal != 0 && d->causal != 1) OMNI_FAIL(OMNI_ERR_INVALID, "causal must be 0 or 1");
+  if (!(d->softmax_scale > 0.f) || !std::isfinite(d->softmax_scale))
+    OMNI_FAIL(OMNI_ERR_INVALID, "softmax_scale must be positive and finite");
+  if ((long long)d->batch * d->n_q_heads > 65535 || (long long)d->batch * d->n_kv_heads > 65535)
+    OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "batch * heads must be at most 65535");
+  if ((long long)d->batch * d->n_q_heads * (long long)d->n_new >= (1ll << 31))
+    OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "batch * n_q_heads * n_new must be below 2^31");
+  for (int k = 0; k < 3; ++k) {
+    if (d->q_stride[k] % 8 || d->kv_stride[k] % 8) OMNI_FAIL(OMNI_ERR_INVALID, "strides must be multiples of 8 elements");
+    if (d->q_stride[k] < d->head_dim || d->kv_stride[k] < d->head_dim)
+      OMNI_FAIL(OMNI_ERR_INVALID, "strides must be at least head_dim");
+  }
+  return OMNI_OK;
+}
+
+static int validate_rope(const omni_rope_desc* r, int head_dim) {
+  if (!r) OMNI_FAIL(OMNI_ERR_INVALID, "rope descriptor is null");
+  if (r->head_dim != head_dim) OMNI_FAIL(OMNI_ERR_INVALID, "rope: head_dim differs from the layer's");
+  if (r->rot_dim < 16 || r->rot_dim > r->head_dim || r->rot_dim % 16)
+    OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "rope: rot_dim must be a multiple of 16 in [16, head_dim]");
+  if (r->interleaved != 0 && r->interleaved != 1) OMNI_FAIL(OMNI_ERR_INVALID, "rope: interleaved must be 0 or 1");
+  if (!std::isfinite(r->out_scale)) OMNI_FAIL(OMNI_ERR_INVALID, "rope: out_scale must be finite");
+  for (int i = 0; i < r->rot_dim / 2; ++i)
+    if (!std::isfinite(r->inv_freq[i]) || std::fabs(r->inv_freq[i]) > 1e6)
+      OMNI_FAIL(OMNI_ERR_INVALID, "rope: inv_freq must be finite and at most 1e6 (not filled by omni_rope_frequencies?)");
+  return OMNI_OK;
+}
+
+static Chunk make_chunk(const omni_chunk_desc* d) {
+  Chunk c;
+  c.B = d->batch;
+  c.Hq = d->n_q_heads;
+  c.Hkv = d->n_kv_heads;
+  c.G = c.Hq / c.Hkv;
+  c.D = d->head_dim;
+  c.n_new = d->n_new;
+  c.causal = d->causal;
+  c.scale = d->softmax_scale;
+  for (int k = 0; k < 3; ++k) {
+    c.qs[k] = d->q_stride[k];
+    c.ks[k] = d->kv_stride[k];
+  }
+  return c;
 }
 
 int check_ws(const void* ws, size_t have, size_t need) {
@@ -392,6 +445,13 @@ size_t omni_workspace_bytes(int call_id, const void* desc, int32_t param) {
     const omni_decode_desc* d = static_cast<const omni_decode_desc*>(desc);
     if (validate_decode(d) != OMNI_OK) return 0;
     return decode_ws(d) + (call_id == OMNI_CALL_SLIM_DECODE ? static_lists_bytes(d) : 0);
+  }
+  if (call_id == OMNI_CALL_PAGED_ATTN || call_id == OMNI_CALL_PAGED_EVICT) {
+    const omni_chunk_desc* d = static_cast<const omni_chunk_desc*>(desc);
+    if (validate_chunk(d) != OMNI_OK) return 0;
+    if (param < 0) { set_error("rows_cap must not be negative"); return 0; }
+    return call_id == OMNI_CALL_PAGED_ATTN ? paged_attn_ws(make_chunk(d), d->dtype, param)
+                                           : paged_evict_ws(d->batch * d->n_kv_heads, param);
   }
   const omni_layer_desc* d = static_cast<const omni_layer_desc*>(desc);
   if (validate_layer(d) != OMNI_OK) return 0;
@@ -998,6 +1058,111 @@ int omni_slim_decode_paged(const omni_decode_desc* desc, const void* q, const vo
   CHECK(check_ws(ws, ws_bytes, decode_ws(desc)));
   return run_decode(desc, q, Kcache, Vcache, ctx_len, probe_keys, grp_idx, grp_cnt, grp_mask, u_cap, O, active, ws,
                     static_cast<hipStream_t>(stream), pool->K, pool->V, &pp);
+}
+
+int omni_rope_frequencies(omni_rope_desc* rope, double base, int scaling, double factor, double orig_len, double low_turns,
+                          double high_turns) {
+  clear_error();
+  REQUIRE_PTR(rope);
+  if (rope->head_dim != 64 && rope->head_dim != 128) OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  if (!(base > 1.0) || !std::isfinite(base)) OMNI_FAIL(OMNI_ERR_INVALID, "base must be finite and above 1");
+  if (scaling < 0 || scaling > 2) OMNI_FAIL(OMNI_ERR_INVALID, "scaling must be 0, 1 or 2");
+  if (scaling && (!(factor > 0.0) || !std::isfinite(factor))) OMNI_FAIL(OMNI_ERR_INVALID, "factor must be positive and finite");
+  if (scaling == 2 && (!(orig_len > 0.0) || !std::isfinite(orig_len) || !(low_turns < high_turns) ||
+                       !std::isfinite(low_turns) || !std::isfinite(high_turns)))
+    OMNI_FAIL(OMNI_ERR_INVALID, "need orig_len > 0 and low_turns < high_turns");
+  omni_rope_desc r = *rope;
+  if (r.rot_dim < 16 || r.rot_dim > r.head_dim || r.rot_dim % 16)
+    OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "rope: rot_dim must be a multiple of 16 in [16, head_dim]");
+  for (int i = 0; i < r.rot_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / r.rot_dim);
+    if (scaling == 1) f /= factor;
+    if (scaling == 2) {
+      const double turns = orig_len * f / 6.283185307179586;
+      const double keep = std::min(1.0, std::max(0.0, (turns - low_turns) / (high_turns - low_turns)));
+      f *= keep + (1.0 - keep) / factor;
+    }
+    r.inv_freq[i] = f;
+  }
+  CHECK(validate_rope(&r, r.head_dim));
+  *rope = r;
+  return OMNI_OK;
+}
+
+int omni_rope(const omni_rope_desc* rope, const omni_layer_desc* desc, const void* Q, const void* K, const int32_t* pos,
+              int backward, void* Qout, void* Kout, void* stream) {
+  clear_error();
+  CHECK(validate_layer(desc));
+  CHECK(validate_rope(rope, desc->head_dim));
+  REQUIRE_PTR(Q); REQUIRE_PTR(K); REQUIRE_PTR(Qout); REQUIRE_PTR(Kout);
+  REQUIRE_ALIGNED(Q); REQUIRE_ALIGNED(K); REQUIRE_ALIGNED(Qout); REQUIRE_ALIGNED(Kout);
+  if (backward != 0 && backward != 1) OMNI_FAIL(OMNI_ERR_INVALID, "backward must be 0 or 1");
+  if (desc->batch > 65535) OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "batch must be at most 65535");
+  return run_rope(*rope, make_layer(desc), desc->dtype, Q, K, pos, backward != 0, Qout, Kout, static_cast<hipStream_t>(stream));
+}
+
+static int validate_pages(const omni_page_pool* pool, Pages* out) {
+  PagePool pp;
+  CHECK(validate_pool(pool, 1, &pp));
+  if ((long long)pool->pages_cap * pool->page_rows >= (1ll << 31))
+    OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "pool: pages_cap * page_rows must be below 2^31");
+  *out = Pages{pool->K, pool->V, pool->page_table, pp.page_shift, pool->pages_cap, pool->n_pages};
+  return OMNI_OK;
+}
+
+int omni_paged_append(const omni_chunk_desc* desc, const omni_rope_desc* rope, const void* Q, const void* K, const void* V,
+                      const omni_page_pool* pool, const int32_t* pos, const int32_t* new_cnt, const int32_t* row_cnt,
+                      void* Qout, int32_t* row_end, int32_t* row_pos, float* acc, void* stream) {
+  clear_error();
+  CHECK(validate_chunk(desc));
+  if (rope) {
+    CHECK(validate_rope(rope, desc->head_dim));
+    REQUIRE_PTR(Q); REQUIRE_PTR(Qout);
+  } else if (Q || Qout) {
+    OMNI_FAIL(OMNI_ERR_INVALID, "Q and Qout are for calls with rope");
+  }
+  REQUIRE_PTR(K); REQUIRE_PTR(V); REQUIRE_PTR(pos); REQUIRE_PTR(new_cnt); REQUIRE_PTR(row_cnt); REQUIRE_PTR(row_end);
+  REQUIRE_PTR(row_pos);
+  REQUIRE_ALIGNED(Q); REQUIRE_ALIGNED(Qout); REQUIRE_ALIGNED(K); REQUIRE_ALIGNED(V);
+  if (row_cnt == row_end) OMNI_FAIL(OMNI_ERR_INVALID, "row_end must not be row_cnt: the launch reads one while it writes the other");
+  Pages pg;
+  CHECK(validate_pages(pool, &pg));
+  return run_paged_append(make_chunk(desc), desc->dtype, rope, Q, K, V, pg, pos, new_cnt, row_cnt, Qout, row_end, row_pos, acc,
+                          static_cast<hipStream_t>(stream));
+}
+
+int omni_paged_attn(const omni_chunk_desc* desc, const void* Q, const omni_page_pool* pool, const int32_t* row_end,
+                    const int32_t* new_cnt, void* O, float* lse, const float* acc_in, float* acc_out, void* ws, size_t ws_bytes,
+                    void* stream) {
+  clear_error();
+  CHECK(validate_chunk(desc));
+  REQUIRE_PTR(Q); REQUIRE_PTR(row_end); REQUIRE_PTR(new_cnt); REQUIRE_PTR(O); REQUIRE_PTR(lse);
+  REQUIRE_ALIGNED(Q); REQUIRE_ALIGNED(O);
+  if (acc_in && !acc_out) OMNI_FAIL(OMNI_ERR_INVALID, "acc_in without acc_out");
+  if (O == Q) OMNI_FAIL(OMNI_ERR_INVALID, "O must not be Q");
+  Pages pg;
+  CHECK(validate_pages(pool, &pg));
+  if (pool->page_rows < 16) OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "pool: page_rows must be at least 16");
+  const Chunk c = make_chunk(desc);
+  CHECK(check_ws(ws, ws_bytes, paged_attn_ws(c, desc->dtype, acc_out ? rows_cap(pg) : 0)));
+  return run_paged_attn(c, desc->dtype, Q, pg, row_end, new_cnt, O, lse, acc_in, acc_out, ws, static_cast<hipStream_t>(stream));
+}
+
+int omni_paged_evict(const omni_chunk_desc* desc, const omni_page_pool* pool, int32_t budget, int32_t n_sink, int32_t n_recent,
+                     const int32_t* seq_len, const int32_t* row_end, const int32_t* row_pos, const float* acc, int32_t* row_cnt,
+                     int32_t* row_pos_out, float* acc_out, void* ws, size_t ws_bytes, void* stream) {
+  clear_error();
+  CHECK(validate_chunk(desc));
+  REQUIRE_PTR(seq_len); REQUIRE_PTR(row_end); REQUIRE_PTR(row_pos); REQUIRE_PTR(acc); REQUIRE_PTR(row_cnt);
+  REQUIRE_PTR(row_pos_out); REQUIRE_PTR(acc_out);
+  if (n_sink < 0 || n_recent < 0) OMNI_FAIL(OMNI_ERR_INVALID, "n_sink and n_recent must not be negative");
+  if (budget < 1 || (long long)n_sink + n_recent > budget)
+    OMNI_FAIL(OMNI_ERR_INVALID, "budget must be at least 1 and n_sink + n_recent");
+  Pages pg;
+  CHECK(validate_pages(pool, &pg));
+  CHECK(check_ws(ws, ws_bytes, paged_evict_ws(desc->batch * desc->n_kv_heads, rows_cap(pg))));
+  return run_paged_evict(desc->batch, desc->n_kv_heads, desc->head_dim, desc->dtype, pg, budget, n_sink, n_recent, seq_len, row_end,
+                         row_pos, acc, row_cnt, row_pos_out, acc_out, ws, static_cast<hipStream_t>(stream));
 }
 
 int omni_dense_decode(const omni_decode_desc* desc, const void* q, const void* Kcache, const void* Vcache,
