@@ -651,7 +651,7 @@ int omni_rope(const omni_rope_desc* rope, const omni_layer_desc* desc, const voi
 /*
  * A cache that grows and shrinks in pages (omni_page_pool; here a table entry holds rows
  * [e * page_rows, (e + 1) * page_rows) of its (sequence, KV head) pair, and a pair can hold
- * rows_cap = pages_cap * page_rows rows).  Every row carries its token's position and,
+ * rows_cap = pages_cap * page_rows rows, at most 2^30).  Every row carries its token's position and,
  * where the caller wants to evict by it, the attention weight it has collected:
  *   row_pos [batch, n_kv_heads, rows_cap] i32, acc [batch, n_kv_heads, rows_cap] f32.
  * One step of a serving loop is

@@ -1104,8 +1104,8 @@ int omni_rope(const omni_rope_desc* rope, const omni_layer_desc* desc, const voi
 static int validate_pages(const omni_page_pool* pool, Pages* out) {
   PagePool pp;
   CHECK(validate_pool(pool, 1, &pp));
-  if ((long long)pool->pages_cap * pool->page_rows >= (1ll << 31))
-    OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "pool: pages_cap * page_rows must be below 2^31");
+  if ((long long)pool->pages_cap * pool->page_rows > (1ll << 30))
+    OMNI_FAIL(OMNI_ERR_UNSUPPORTED, "pool: pages_cap * page_rows must be at most 2^30");
   *out = Pages{pool->K, pool->V, pool->page_table, pp.page_shift, pool->pages_cap, pool->n_pages};
   return OMNI_OK;
 }

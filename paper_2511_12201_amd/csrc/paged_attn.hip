@@ -1,258 +1,663 @@
-// Attention of a chunk of new tokens over a paged cache (omni_paged_attn), and the weight that every row collects by it.
+// Attention of a chunk of new tokens over a paged cache (omni_paged_attn) in bf16, and what joins split items in both types.
 //
-// The query heads of a KV head share its rows, so the unit of work is a pair (sequence, KV head) with G * new_cnt query rows:
-// row r is token r / G, head r % G of the group.  Both products are formed transposed, S^T = K Q^T and O^T = V^T P^T: a lane
-// owns one query row, the softmax statistics are per-lane scalars and the accumulators of S^T are the B operand of the second
-// product as they stand.  Running maximum and sum, one pass over the rows; rows that are not there (behind the last one, or on a
-// page that is missing) are read as zeros and masked.
-#include "paged.h"
+// The query heads of a KV head share its rows, so the unit of work is a pair (sequence, KV head) with G * new_cnt query rows.
+// Both products are formed transposed, S^T = K Q^T and O^T = V^T P^T, with 32x32x16 matrix instructions: a lane owns one query
+// row, the softmax statistics are per-lane scalars and the accumulators of S^T are the second product's B operand as they stand.
+// Running maximum and sum, one pass over the rows.  Rows that are not there (behind the last one, or on a page that is missing)
+// enter as zeros and are masked.
+//
+//  * Few query rows a pair (paged_stream_kernel, at most 32): memory bounds it.  A wavefront takes 32 cache rows per trip, K
+//    straight from memory in fragment layout, V through a tile of its own that is read back transposed; no barrier in the loop.
+//  * Many (paged_tile_kernel): eight wavefronts of 32 query rows share 64-row tiles that go from the pages straight into a ring
+//    of four LDS stages, one barrier a tile; the softmax of a tile runs under the matrix instructions of the next.
+// The weights are rounded to bf16 for the second product (half a step: 2^-8 relative each, the errors of many rows average out);
+// their sum is taken before the rounding, in fp32.
+#include "paged_dev.h"
+
+#include <type_traits>
 
 namespace omni {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-struct AttnParams {
-  const void* Q;
-  void* O;
-  float* lse;
-  Pages pg;
-  const int *row_end, *new_cnt;
-  const float* acc_in;
-  float* acc_out;
-  Chunk c;
-};
+// ------------------------------------------------------------------ few query rows: stream the cache
 
-// Query rows and cache rows of a pair, and how many rows a query row sees.
-struct PairView {
-  int pair, b, g, cnt, end, M;
-  __device__ __forceinline__ PairView(const AttnParams& p, int pair_) : pair(pair_) {
-    b = pair / p.c.Hkv;
-    g = pair - b * p.c.Hkv;
-    cnt = clampi(p.new_cnt[b], 0, p.c.n_new);
-    end = clampi(p.row_end[pair], 0, rows_cap(p.pg));
-    M = cnt * p.c.G;
-  }
-  __device__ __forceinline__ int visible(const AttnParams& p, int t) const { return p.c.causal ? max(end - cnt + t + 1, 0) : end; }
-};
+constexpr int kStreamWaves = 4, kStreamThreads = kStreamWaves * 64, kStreamRows = 32;
 
-template <typename T>
-__device__ __forceinline__ float to_f32(T x);
-template <>
-__device__ __forceinline__ float to_f32<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ float to_f32<u16>(u16 x) { return bf16_bits_to_f32(x); }
-
-// Rows [j0, j0 + ROWS) of a pair as fp32 into LDS, pitch D + 4; what is not there as zeros.  Returns nothing; `there` gets a bit
-// per row (ROWS = 32).
-template <typename T, int D, int THREADS>
-__device__ __forceinline__ void stage_rows(const Pages& pg, const void* store, int pair, int end, int j0, float* dst) {
-  constexpr int E = Elem<T>::kPer16B, CPR = D / E;
-  for (int i = threadIdx.x; i < 32 * CPR; i += THREADS) {
-    const int r = i / CPR, c = i % CPR, j = j0 + r;
-    const int row = j < end ? pool_row(pg, pair, j) : -1;
-    float x[E];
-    u32x4 raw = {0u, 0u, 0u, 0u};
-    if (row >= 0) raw = *reinterpret_cast<const u32x4*>(static_cast<const T*>(store) + (long long)row * D + c * E);
-    unpack16(raw, x, (const T*)nullptr);
-#pragma unroll
-    for (int e = 0; e < E; e += 4) *reinterpret_cast<f32x4*>(dst + r * (D + 4) + c * E + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-  }
-}
-
-constexpr int kWaves = 4, kThreads = kWaves * 64, kRows = kWaves * 32;
-
-// grid: (blocks of kRows query rows, pairs)
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void paged_attn_f32_kernel(AttnParams p) {
-  __shared__ float sK[32 * (D + 4)], sV[32 * (D + 4)];
-  __shared__ unsigned sThere;
+template <int D, bool LOGITS>
+__global__ __launch_bounds__(kStreamThreads, 3) void paged_stream_kernel(AttnParams p) {
+  constexpr int CPR = D / 8, RPI = 64 / CPR, NVL = 32 / RPI, NB = D / 32;
+  constexpr int VP = D * 2 + 16;                         // bytes between rows of a V tile and of the queries
+  constexpr int OP = 36;                                 // floats between the rows of the merge buffer (32 of the D elements at a time)
+  __shared__ __attribute__((aligned(16))) unsigned char sV[kStreamWaves * 32 * VP], sQ[32 * VP];
+  __shared__ float sM[kStreamWaves][32], sL[kStreamWaves][32];
+  __shared__ Scan scan;
+  static_assert(kStreamWaves * 32 * OP * 4 <= (int)sizeof(sV), "the merge buffer takes the V tiles' place");
   const Chunk& c = p.c;
-  const PairView w(p, blockIdx.y);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, ln = lane & 31, h = lane >> 5;
-  const int r = blockIdx.x * kRows + wave * 32 + ln;
-  const int t = r / c.G, head = w.g * c.G + r % c.G;
-  const bool in_chunk = t < c.n_new, real = t < w.cnt;
-  const int vis = real ? w.visible(p, t) : 0;
-  const int r_last = min((int)(blockIdx.x + 1) * kRows, w.M) - 1;
-  const int keys = r_last >= (int)blockIdx.x * kRows ? w.visible(p, r_last / c.G) : 0;
-
-  float q[D / 2];
-#pragma unroll
-  for (int k = 0; k < D / 2; ++k) q[k] = 0.f;
-  const long long qoff = w.b * c.qs[0] + head * c.qs[1] + (long long)t * c.qs[2];
-  if (real) {
-    const T* src = static_cast<const T*>(p.Q) + qoff + h * (D / 2);
-#pragma unroll
-    for (int k = 0; k < D / 2; ++k) q[k] = to_f32<T>(src[k]);
-  }
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id(), n = lane & 31, h = lane >> 5;
   const float c2 = c.scale * kLog2e;
-  f32x16 o[D / 32];
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
-  float m = -INFINITY, l = 0.f;
+  unsigned char* tile = sV + wave * 32 * VP;
+  // transposing reads: a lane supplies four neighbours of one row and gets four rows of one column, in the order in which the
+  // accumulators hold the weights
+  typedef __attribute__((address_space(3))) s16x4* lds_quads;
+  const lds_quads vcol = (lds_quads)(tile + (4 * h + (n & 15) / 4) * VP + (n & 16) * 2 + (n & 3) * 8);
+  const unsigned char* qlane = sQ + n * VP + h * 16;
+  const u16* Kp = static_cast<const u16*>(p.pg.K);
+  const u16* Vp = static_cast<const u16*>(p.pg.V);
 
-  for (int j0 = 0; j0 < keys; j0 += 32) {
+  for_segments<kStreamThreads>(p, scan, blockIdx.x, [&](const Segment& seg) {
+    const PairView w(p, seg.pair);
+    __syncthreads();                                     // the last segment's queries and merge buffer are done with
+    for (int i = threadIdx.x; i < 32 * CPR; i += kStreamThreads) {
+      const int r = i / CPR;
+      u32x4 raw = {0u, 0u, 0u, 0u};
+      if (r < w.M) {
+        long long at_lse;
+        raw = *reinterpret_cast<const u32x4*>(static_cast<const u16*>(p.Q) + out_row(p, w, r, at_lse) + i % CPR * 8);
+      }
+      *reinterpret_cast<u32x4*>(sQ + r * VP + i % CPR * 16) = raw;
+    }
+    const int vis = n < w.M ? w.visible(p, n / c.G) : 0;
+    const int keys = w.visible(p, (w.M - 1) / c.G);
+    f32x16 o[NB];
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    const int first = seg.u0 * kStreamWaves + wave, last = min(seg.u1 * kStreamWaves, cdiv(keys, 32));
+    auto row_of = [&](int block) {
+      const int j = block * 32 + n;
+      return block < last && j < w.end ? pool_row(p.pg, w.pair, j) : -1;
+    };
+    int row = row_of(first);
     __syncthreads();
-    stage_rows<T, D, kThreads>(p.pg, p.pg.K, w.pair, w.end, j0, sK);
-    stage_rows<T, D, kThreads>(p.pg, p.pg.V, w.pair, w.end, j0, sV);
-    if (wave == 0) {
-      const bool is = lane < 32 && j0 + lane < w.end && pool_row(p.pg, w.pair, j0 + lane) >= 0;
-      const unsigned bits = (unsigned)__ballot(is);
-      if (lane == 0) sThere = bits;
-    }
-    __syncthreads();
-    f32x16 s;
+    for (int block = first; block < last; block += kStreamWaves) {
+      bf16x8 kf[D / 16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+      for (int ks = 0; ks < D / 16; ++ks) {
+        u32x4 raw = {0u, 0u, 0u, 0u};
+        if (row >= 0) raw = *reinterpret_cast<const u32x4*>(Kp + (long long)row * D + ks * 16 + h * 8);
+        kf[ks] = __builtin_bit_cast(bf16x8, raw);
+      }
+      u32x4 vraw[NVL];
 #pragma unroll
-    for (int k = 0; k < D / 2; k += 4) {
-      const f32x4 kv = *reinterpret_cast<const f32x4*>(sK + ln * (D + 4) + h * (D / 2) + k);
+      for (int j = 0; j < NVL; ++j) {
+        const int vr = __shfl(row, j * RPI + lane / CPR, 64);
+        vraw[j] = u32x4{0u, 0u, 0u, 0u};
+        if (vr >= 0) vraw[j] = *reinterpret_cast<const u32x4*>(Vp + (long long)vr * D + (lane % CPR) * 8);
+      }
+      const unsigned there = (unsigned)__ballot(row >= 0) >> (4 * h);
+      row = row_of(block + kStreamWaves);                // a row's address depends on its table entry: fetched a trip ahead
+      f32x16 s;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[e], q[k + e], s, 0, 0, 0);
-    }
-    const unsigned there = sThere >> (4 * h);
-    float mx = m;
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int key = 8 * (i / 4) + i % 4;                        // + 4 h
-      s[i] = j0 + 4 * h + key < vis && ((there >> key) & 1u) ? s[i] * c2 : -INFINITY;
-      mx = fmaxf(mx, s[i]);
-    }
-    mx = pair_max(mx);
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    const float alpha = fast_exp2(m - ref);
-    float sum = 0.f;
+      for (int ks = 0; ks < D / 16; ++ks)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], *reinterpret_cast<const bf16x8*>(qlane + ks * 32), s, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[i] = fast_exp2(s[i] - ref);
-      sum += s[i];
-    }
-    l = fmaf(l, alpha, sum);
-    m = mx;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+      for (int j = 0; j < NVL; ++j)
+        *reinterpret_cast<u32x4*>(tile + (j * RPI + lane / CPR) * VP + (lane % CPR) * 16) = vraw[j];
+      const int rel = vis - block * 32 - 4 * h;          // rows of this block from here on are not seen
+      float mx = m;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float v = sV[(8 * (i / 4) + 4 * h + i % 4) * (D + 4) + db * 32 + ln];
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i], o[db], 0, 0, 0);
+        const int key = 8 * (i / 4) + i % 4;             // + 4 h
+        s[i] = key < rel && ((there >> key) & 1u) ? s[i] * c2 : -INFINITY;
+        mx = fmaxf(mx, s[i]);
+      }
+      if constexpr (LOGITS) {
+        if (n < w.M) {
+          const int mfull = c.G * c.n_new;
+          float* dst = p.logits + (((long long)w.pair * cdiv(rows_cap(p.pg), 32) + block) * mfull + n) * 32 + 4 * h;
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(dst + 2 * i) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
+        }
+      }
+      mx = pair_max(mx);
+      const float ref = mx == -INFINITY ? 0.f : mx;
+      const float alpha = mx == m ? 1.f : fast_exp2(m - ref);
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[i] = fast_exp2(s[i] - ref);
+        sum += s[i];
+      }
+      l = fmaf(l, alpha, sum);
+      m = mx;
+      if (__any(alpha != 1.f)) {
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+      }
+      union { bf16x8 v[2]; unsigned u[8]; } pf;
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) pf.u[i / 2] = pack_bf16x2(s[i], s[i + 1]);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the tile is this wavefront's own: its writes are done
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+        for (int db = 0; db < NB; ++db) {
+          union { s16x4 q[2]; bf16x8 v; } vf;
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+            vf.q[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vcol + ((16 * s2 + 8 * half) * VP + 64 * db) / 8);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf.v[s2], o[db], 0, 0, 0);
+        }
+    }
+    // join the wavefronts in their order, 32 elements of the rows at a time
+    const float own = pair_sum(l);
+    if (h == 0) {
+      sM[wave][n] = m;
+      sL[wave][n] = own;
+    }
+    __syncthreads();
+    float top = sM[0][n];
+#pragma unroll
+    for (int v = 1; v < kStreamWaves; ++v) top = fmaxf(top, sM[v][n]);
+    const float ref = top == -INFINITY ? 0.f : top, mine = fast_exp2(m - ref);
+    float total = 0.f;
+#pragma unroll
+    for (int v = 0; v < kStreamWaves; ++v) total = fmaf(sL[v][n], fast_exp2(sM[v][n] - ref), total);
+    const float inv = total > 0.f ? 1.f / total : 0.f;
+    if (wave == 0 && h == 0 && n < w.M) {
+      if (seg.whole) {
+        long long at_lse;
+        out_row(p, w, n, at_lse);
+        p.lse[at_lse] = total > 0.f ? (top + log2f(total)) * kLn2 : -INFINITY;
+      } else {
+        *reinterpret_cast<f32x2*>(p.part_ml + ((long long)seg.slot * kStreamRows + n) * 2) = f32x2{top, total};
       }
     }
-  }
-  if (!in_chunk) return;
-  const float total = pair_sum(l), inv = total > 0.f ? 1.f / total : 0.f;
-  T* dst = static_cast<T*>(p.O) + qoff;
+    const float by = seg.whole ? mine * inv : mine;
+    float* sO = reinterpret_cast<float*>(sV);
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db)
+    for (int db = 0; db < NB; ++db) {
+      __syncthreads();                                   // tiles, or the elements before, are done with
 #pragma unroll
-    for (int i = 0; i < 16; ++i) Elem<T>::store(dst + db * 32 + 8 * (i / 4) + 4 * h + i % 4, o[db][i] * inv);
-  if (h == 0) p.lse[((long long)w.b * c.Hq + head) * c.n_new + t] = total > 0.f ? (m + log2f(total)) * kLn2 : -INFINITY;
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<f32x4*>(sO + (wave * 32 + n) * OP + 2 * i + 4 * h) = f32x4{o[db][i] * by, o[db][i + 1] * by, o[db][i + 2] * by, o[db][i + 3] * by};
+      __syncthreads();
+      const int r = threadIdx.x / 8, d = threadIdx.x % 8 * 4;
+      if (r < w.M) {
+        f32x4 x = *reinterpret_cast<const f32x4*>(sO + r * OP + d);
+#pragma unroll
+        for (int v = 1; v < kStreamWaves; ++v) x += *reinterpret_cast<const f32x4*>(sO + (v * 32 + r) * OP + d);
+        if (seg.whole) {
+          long long at_lse;
+          u16* dst = static_cast<u16*>(p.O) + out_row(p, w, r, at_lse) + db * 32 + d;
+          *reinterpret_cast<uint2*>(dst) = uint2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+        } else {
+          *reinterpret_cast<f32x4*>(p.part_o + ((long long)seg.slot * kStreamRows + r) * D + db * 32 + d) = x;
+        }
+      }
+    }
+  });
 }
 
-// Weights from the finished log-sum-exps: a wavefront owns 32 cache rows, all query rows of the pair pass by.
-// grid: (blocks of kRows cache rows, pairs)
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void paged_weights_f32_kernel(AttnParams p) {
-  __shared__ float sQ[32 * (D + 4)], sL[32];
-  __shared__ int sVis[32];
-  const Chunk& c = p.c;
-  const PairView w(p, blockIdx.y);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, ln = lane & 31, h = lane >> 5;
-  const int j0 = blockIdx.x * kRows + wave * 32;
-  if ((int)blockIdx.x * kRows >= w.end) return;
-  const int row = j0 + ln < w.end ? pool_row(p.pg, w.pair, j0 + ln) : -1;
-  const unsigned there = (unsigned)__ballot(row >= 0) >> (4 * h);
-  float k[D / 2];
-#pragma unroll
-  for (int e = 0; e < D / 2; ++e) k[e] = 0.f;
-  if (row >= 0) {
-    const T* src = static_cast<const T*>(p.pg.K) + (long long)row * D + h * (D / 2);
-#pragma unroll
-    for (int e = 0; e < D / 2; ++e) k[e] = to_f32<T>(src[e]);
+int launch_stream(const AttnParams& p, hipStream_t st) {
+  if (p.c.D == 128) {
+    if (p.logits) paged_stream_kernel<128, true><<<p.n_wgs, kStreamThreads, 0, st>>>(p);
+    else paged_stream_kernel<128, false><<<p.n_wgs, kStreamThreads, 0, st>>>(p);
+  } else {
+    if (p.logits) paged_stream_kernel<64, true><<<p.n_wgs, kStreamThreads, 0, st>>>(p);
+    else paged_stream_kernel<64, false><<<p.n_wgs, kStreamThreads, 0, st>>>(p);
   }
-  const float c2 = c.scale * kLog2e;
-  float sum[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-  constexpr int E = Elem<T>::kPer16B, CPR = D / E;
-  for (int r0 = 0; r0 < w.M; r0 += 32) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < 32 * CPR; i += kThreads) {
-      const int r = r0 + i / CPR, cc = i % CPR, t = r / c.G, head = w.g * c.G + r % c.G;
-      u32x4 raw = {0u, 0u, 0u, 0u};
-      if (r < w.M)
-        raw = *reinterpret_cast<const u32x4*>(static_cast<const T*>(p.Q) + w.b * c.qs[0] + head * c.qs[1] + t * c.qs[2] + cc * E);
-      float x[E];
-      unpack16(raw, x, (const T*)nullptr);
-#pragma unroll
-      for (int e = 0; e < E; ++e) sQ[(i / CPR) * (D + 4) + cc * E + e] = x[e];
-    }
-    if (threadIdx.x < 32) {
-      const int r = r0 + threadIdx.x, t = r / c.G, head = w.g * c.G + r % c.G;
-      const float lse = r < w.M ? p.lse[((long long)w.b * c.Hq + head) * c.n_new + t] : -INFINITY;
-      sL[threadIdx.x] = lse * kLog2e;
-      sVis[threadIdx.x] = lse > -INFINITY ? w.visible(p, t) : 0;
-    }
-    __syncthreads();
-    f32x16 s;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-    for (int e = 0; e < D / 2; e += 4) {
-      const f32x4 q = *reinterpret_cast<const f32x4*>(sQ + ln * (D + 4) + h * (D / 2) + e);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e + x], q[x], s, 0, 0, 0);
-    }
-    const int vis = sVis[ln];
-    const float ref = sL[ln];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int key = 8 * (i / 4) + i % 4;
-      if (j0 + 4 * h + key < vis && ((there >> key) & 1u)) sum[i] += fast_exp2(fmaf(s[i], c2, -ref));
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    float v = sum[i];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    const int j = j0 + 8 * (i / 4) + 4 * h + i % 4;
-    if (ln == 0 && j < w.end) {
-      const long long at = (long long)w.pair * rows_cap(p.pg) + j;
-      p.acc_out[at] = (p.acc_in ? p.acc_in[at] : 0.f) + v;
-    }
-  }
-}
-
-template <typename T, int D>
-int launch(const AttnParams& p, hipStream_t st) {
-  const int pairs = p.c.B * p.c.Hkv;
-  paged_attn_f32_kernel<T, D><<<dim3(cdiv(p.c.G * p.c.n_new, kRows), pairs), kThreads, 0, st>>>(p);
   OMNI_LAUNCH_CHECK();
-  if (p.acc_out) {
-    paged_weights_f32_kernel<T, D><<<dim3(cdiv(rows_cap(p.pg), kRows), pairs), kThreads, 0, st>>>(p);
-    OMNI_LAUNCH_CHECK();
-  }
   return OMNI_OK;
+}
+
+// ------------------------------------------------------------------ many query rows: tiles in LDS
+
+// 512 threads = 8 wavefronts x 32 query rows.  K and V tiles of 64 rows go from the pages straight into LDS (global_load_lds), row by
+// row: an instruction takes 4 (D = 128) or 8 (D = 64) whole rows, which lie in one page (page_rows >= 16), so that a page costs
+// one wave-uniform table entry.  A row's 16-byte pieces change places inside the row as they are written (the lanes' addresses do
+// it): K piece c of row r goes to c ^ (r % 16) (D = 64: c ^ (r / 2 % 8)), so that the 16 lanes that read one piece of 16 rows meet every bank once; V
+// piece c to c ^ 4 (r % 4) (D = 64: c ^ 4 (r / 2 % 2)), so that the transposing reads of 4 rows do.  Ring of four stages, so up to three tiles are in flight
+// while one is computed and one barrier per tile is enough; the waits are counted by hand (the compiler would wait for every
+// load in flight).  Tiles that are not whole (the last one, missing pages) are copied through registers with zeros for what is
+// not there.
+constexpr int kTileWaves = 8, kTileThreads = kTileWaves * 64, kTileRows = kTileWaves * 32;
+constexpr int kTileKeys = 64, kStages = 4;
+constexpr int kTab = 2048;                               // page table entries in LDS: 512 tiles of the smallest pages
+
+template <int D>
+__global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams p) {
+  constexpr int kKBytes = kTileKeys * D * 2, kStageBytes = 2 * kKBytes;
+  constexpr int LPH = kKBytes / 1024 / kTileWaves, LPT = 2 * LPH;     // load instructions per wavefront: of K, of a tile
+  constexpr int RB = D * 2, CPR = D / 8, RPI = 1024 / RB;             // bytes and pieces of a row, rows of a load instruction
+  constexpr int NB = D / 32, KS = D / 16;
+  constexpr int NQK = 2 * KS, NPV = 4 * NB;                           // matrix instructions of the two products of a tile
+  constexpr int kAhead = 2;                                           // fragments are read this many of them ahead
+  static_assert(LPH >= 1 && 32 % NQK == 0 && 32 % NPV == 0, "chunking of the copies and of the vector work");
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kStages * kStageBytes];
+  __shared__ int sTab[kTab];
+  __shared__ int sMissing;
+  __shared__ Scan scan;
+  const Chunk& c = p.c;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), ln = lane & 31, h = lane >> 5;
+  const float c2 = c.scale * kLog2e;
+  const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
+  const unsigned char* Kpool = static_cast<const unsigned char*>(p.pg.K);
+  const unsigned char* Vpool = static_cast<const unsigned char*>(p.pg.V);
+  auto swz_k = [](int row) { return D == 128 ? row & 15 : row >> 1 & 7; };
+  auto swz_v = [](int row) { return D == 128 ? (row & 3) << 2 : (row & 2) << 1; };
+
+  // a lane's source inside the rows that an instruction takes (the instruction's first row is a multiple of RPI = 4 or 8; for K
+  // the row's low bits beyond that are the wavefront's)
+  const int in_row = lane / CPR, slot = lane % CPR;
+  const unsigned src_k = in_row * RB + ((slot ^ swz_k(wave * RPI + in_row)) * 16);
+  const unsigned src_v = in_row * RB + ((slot ^ swz_v(in_row)) * 16);
+  // a lane's fragments: K row ln (+ 32), piece 2 ks + h; V rows 4 h + .. (+ 8, 16 t), 16 bytes of a column group
+  const unsigned frag_k = ln * RB + ((h ^ swz_k(ln)) * 16);
+  const unsigned frag_v = kKBytes + (4 * h + (ln & 15) / 4) * RB + ((swz_v((ln & 15) / 4) + (ln >> 4) * 2) * 16) + (ln & 3) * 8;
+  typedef __attribute__((address_space(3))) s16x4* lds_quads;
+  typedef __attribute__((address_space(3))) bf16x8* lds_eights;
+  const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+
+  for_segments<kTileThreads>(p, scan, blockIdx.x, [&](const Segment& seg) {
+    const PairView w(p, seg.pair);
+    const bool active = seg.r0 + wave * 32 < w.M;        // wave-uniform: the others only copy
+    const int r = seg.r0 + wave * 32 + ln, rc = min(r, w.M - 1);
+    const int qvis = w.visible(p, rc / c.G) - 4 * h;     // compared with rows of a tile that leave out 4 h
+    const int seen_by_all = w.visible(p, seg.r0 / c.G);
+    long long at_lse;
+    const long long at_row = out_row(p, w, rc, at_lse);
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(static_cast<const u16*>(p.Q) + at_row + ks * 16 + h * 8);
+    // the loads end here: a wait for them inside the loop would wait for the copies in flight, too
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
+
+    f32x16 o[NB];
+#pragma unroll
+    for (int db = 0; db < NB; ++db) o[db] = zero16;
+    float m_run = -INFINITY, l_run = 0.f, mc = 0.f;      // reference value of the weights (mc: times c2, 0 if there is none yet)
+    constexpr float kRescaleSlack = 6.0f;                // it moves when a row exceeds it by this much in the exponent
+    constexpr float kHuge = 1099511627776.f;             // 2^40: fp32 accumulators and bf16 weights are far from their range
+
+    // stretches of the span whose table entries fit the window
+    const int tiles_per_window = max(1, (int)min((long long)(kTab - 1) << p.pg.shift >> 6, (long long)0x3fffffff));
+    for (int c0 = seg.u0, c1; c0 < seg.u1; c0 = c1) {
+      c1 = min(seg.u1, c0 + tiles_per_window);
+      const int nt = c1 - c0;
+      const int tab0 = (c0 * kTileKeys) >> p.pg.shift;
+      const int tab_end = min(cdiv(min(c1 * kTileKeys, w.end), 1 << p.pg.shift), p.pg.pages_cap);
+      __syncthreads();                                   // everyone is done with the stretch before
+      if (threadIdx.x == 0) sMissing = 0;
+      __syncthreads();
+      for (int i = threadIdx.x; i < tab_end - tab0; i += kTileThreads) {
+        const int page = p.pg.table[(long long)seg.pair * p.pg.pages_cap + tab0 + i];
+        const bool there = (unsigned)page < (unsigned)p.pg.n_pages;
+        sTab[i] = there ? page : -1;
+        if (!there) sMissing = 1;
+      }
+      __syncthreads();
+      const bool missing = __builtin_amdgcn_readfirstlane(sMissing) != 0;
+      const int n_plain = missing ? 0 : min(nt, w.end / kTileKeys - c0);              // whole tiles come first
+      const int n_full = missing ? 0 : min(seen_by_all / kTileKeys - c0, nt);         // tiles in which nothing is masked
+
+      auto issue_part = [&](int t, int part) {           // one load instruction of tile c0 + t: part < LPH is K
+        const unsigned dst = lds_base + (unsigned)(t % kStages) * kStageBytes;
+        const bool is_k = part < LPH;
+        const int at = (is_k ? part : part - LPH) * kTileWaves + wave;
+        const int j = (c0 + t) * kTileKeys + at * RPI;
+        const int page = __builtin_amdgcn_readfirstlane(sTab[(j >> p.pg.shift) - tab0]);
+        const long long row = ((long long)page << p.pg.shift) + (j & ((1 << p.pg.shift) - 1));
+        if (is_k) gload_lds16(Kpool + row * RB, src_k, dst + at * 1024);
+        else gload_lds16(Vpool + row * RB, src_v, dst + kKBytes + at * 1024);
+      };
+      auto row_there = [&](int j) { return j < w.end ? sTab[(j >> p.pg.shift) - tab0] : -1; };
+      auto copy_tile = [&](int t) {                      // a tile that is not whole; its loads end here
+        unsigned char* dst = smem + (t % kStages) * kStageBytes;
+        for (int i = threadIdx.x; i < kTileKeys * CPR; i += kTileThreads) {
+          const int row = i / CPR, piece = i % CPR, j = (c0 + t) * kTileKeys + row;
+          const int page = row_there(j);
+          u32x4 k = {0u, 0u, 0u, 0u}, v = k;
+          if (page >= 0) {
+            const long long src = (((long long)page << p.pg.shift) + (j & ((1 << p.pg.shift) - 1))) * RB + piece * 16;
+            k = *reinterpret_cast<const u32x4*>(Kpool + src);
+            v = *reinterpret_cast<const u32x4*>(Vpool + src);
+          }
+          *reinterpret_cast<u32x4*>(dst + row * RB + (piece ^ swz_k(row)) * 16) = k;
+          *reinterpret_cast<u32x4*>(dst + kKBytes + row * RB + (piece ^ swz_v(row)) * 16) = v;
+        }
+      };
+      auto issue_tile = [&](int t) {
+        if (t < n_plain) {
+#pragma unroll
+          for (int j = 0; j < LPT; ++j) issue_part(t, j);
+        } else {
+          copy_tile(t);
+        }
+      };
+      auto kfrag = [&](unsigned stage, int i) {
+        const int kb = i % 2, ks = i / 2;
+        return *(lds_eights)(size_t)(lds_base + ((stage + frag_k) ^ (ks * 32)) + kb * 32 * RB);
+      };
+      auto vfrag = [&](unsigned stage, int i) {
+        const int t16 = i / NB, db = i % NB;
+        const unsigned at = lds_base + ((stage + frag_v) ^ (db * 64)) + t16 * 16 * RB;
+        union { s16x4 q[2]; bf16x8 v; } f;
+        f.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quads)(size_t)at);
+        f.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quads)(size_t)(at + 8 * RB));
+        return f.v;
+      };
+      auto rescale = [&](float mloc) {
+        const float m_new = fmaxf(m_run, mloc);
+        const float m_ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = fast_exp2((m_run - m_ref) * c2);
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+        m_run = m_new;
+        mc = m_ref * c2;
+      };
+      auto tile_max = [&](const f32x16 (&sn)[2]) {
+        float mloc = sn[0][0];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) mloc = fmaxf(fmaxf(sn[kb][i], sn[kb][i + 1]), mloc);
+        return mloc;
+      };
+      auto update_max = [&](float mloc) {
+        mloc = pair_max(mloc);
+        if (__any(mloc > m_run + kRescaleSlack / c2)) rescale(mloc);
+      };
+      auto mask_tile = [&](f32x16 (&sn)[2], int t) {
+        const int rel = qvis - (c0 + t) * kTileKeys;
+        u64 there = ~0ull;
+        if (missing) there = __ballot(row_there((c0 + t) * kTileKeys + lane) >= 0);
+        there >>= 4 * h;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = kb * 32 + 8 * (i / 4) + i % 4;
+            if (key >= rel || !((there >> key) & 1u)) sn[kb][i] = -INFINITY;
+          }
+        return tile_max(sn);
+      };
+      auto weights = [&](const f32x16 (&sc)[2], int i, float& sum) {       // two weights, packed
+        const float a = fast_exp2(fmaf(sc[i / 16][i % 16], c2, -mc)), b = fast_exp2(fmaf(sc[i / 16][i % 16 + 1], c2, -mc));
+        sum += a;
+        sum += b;
+        return pack_bf16x2(a, b);
+      };
+      union PFrag { bf16x8 v[4]; unsigned u[16]; };
+
+      // One step: weights of tile t from sc and O += V(t) P(t); where there is a tile t + 1, its scores into sn under the
+      // weights, and their maximum under the second product.  kSteady: there is one, and tile t + 3 is whole and issued here.
+      // Once every row of the wavefront has a reference value the maximum is not followed any more (kFollow false): the value
+      // can only be too low, and a weight that grows past kHuge shows in the tile's sum.
+      auto step = [&](auto steady, auto follows, f32x16 (&sc)[2], f32x16 (&sn)[2], int t) {
+        constexpr bool kSteady = decltype(steady)::value, kFollow = decltype(follows)::value;
+        const bool has_next = kSteady || t + 1 < nt;
+        const unsigned stage = (unsigned)(t % kStages) * kStageBytes, stage_n = (unsigned)((t + 1) % kStages) * kStageBytes;
+        PFrag pf;
+        float lsum = 0.f;
+        bf16x8 vf[kAhead];
+        constexpr int EQ = 32 / NQK;
+        if (has_next) {
+          if (kSteady || t + 2 < nt) wait_vmcnt<LPT>();  // this wavefront's share of tile t + 1 has landed
+          else wait_vmcnt<0>();
+          __syncthreads();                               // and everyone's; tile t - 1 is done with
+          if (!kSteady && t + 3 < nt) issue_tile(t + 3);
+          __builtin_amdgcn_sched_barrier(0);
+          bf16x8 kf[kAhead];
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) kf[i] = kfrag(stage_n, i);
+#pragma unroll
+          for (int i = 0; i < NQK; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            sn[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % kAhead], qf[i / 2], i < 2 ? zero16 : sn[i % 2], 0, 0, 0);
+            if (i + kAhead < NQK) kf[i % kAhead] = kfrag(stage_n, i + kAhead);
+            else vf[i + kAhead - NQK] = vfrag(stage, i + kAhead - NQK);
+#pragma unroll
+            for (int e = 0; e < EQ; e += 2) pf.u[(i * EQ + e) / 2] = weights(sc, i * EQ + e, lsum);
+            if (kSteady && i * LPH % NQK == 0) issue_part(t + 3, i * LPH / NQK);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) vf[i] = vfrag(stage, i);
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) pf.u[i / 2] = weights(sc, i, lsum);
+        }
+        if (__any(lsum > kHuge)) {
+          rescale(pair_max(tile_max(sc)));
+          lsum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) pf.u[i / 2] = weights(sc, i, lsum);
+        }
+        l_run += lsum;
+        __builtin_amdgcn_s_setprio(0);
+        float mloc = -INFINITY;
+        constexpr int EV = 32 / NPV;
+#pragma unroll
+        for (int i = 0; i < NPV; ++i) {
+          __builtin_amdgcn_sched_barrier(0);
+          o[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % kAhead], pf.v[i / NB], o[i % NB], 0, 0, 0);
+          if (i + kAhead < NPV) vf[i % kAhead] = vfrag(stage, i + kAhead);
+          if constexpr (kFollow) {
+#pragma unroll
+            for (int e = 0; e < EV; e += 2) {
+              const int x = i * EV + e;
+              mloc = fmaxf(fmaxf(sn[x / 16][x % 16], sn[x / 16][x % 16 + 1]), mloc);
+            }
+          }
+          if (kSteady && i * LPH % NPV == 0) issue_part(t + 3, LPH + i * LPH / NPV);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        if (has_next) {
+          if (t + 1 >= n_full) mloc = mask_tile(sn, t + 1);
+          if constexpr (kFollow) update_max(mloc);
+        }
+      };
+
+      // At the top of step t the tiles up to t + 2 have been issued; after its barrier everyone is done with tile t - 1, whose
+      // stage takes tile t + 3.
+      wait_vmcnt<0>();                                   // nothing older is counted below
+      issue_tile(0);
+      if (nt > 1) issue_tile(1);
+      if (nt > 2) issue_tile(2);
+      if (nt > 2) wait_vmcnt<2 * LPT>();
+      else if (nt > 1) wait_vmcnt<LPT>();
+      else wait_vmcnt<0>();
+      __syncthreads();
+      if (active) {
+        f32x16 sa[2], sb[2];
+        sb[0] = zero16;
+        sb[1] = zero16;
+#pragma unroll
+        for (int i = 0; i < NQK; ++i) sa[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kfrag(0, i), qf[i / 2], i < 2 ? zero16 : sa[i % 2], 0, 0, 0);
+        update_max(0 >= n_full ? mask_tile(sa, 0) : tile_max(sa));
+        int t = 0;
+        for (; t + 4 < n_plain && __any(m_run == -INFINITY); t += 2) {      // some row has not seen a cache row yet
+          step(std::true_type{}, std::true_type{}, sa, sb, t);
+          step(std::true_type{}, std::true_type{}, sb, sa, t + 1);
+        }
+        for (; t + 4 < n_plain; t += 2) {
+          step(std::true_type{}, std::false_type{}, sa, sb, t);
+          step(std::true_type{}, std::false_type{}, sb, sa, t + 1);
+        }
+        for (; t < nt; t += 2) {
+          step(std::false_type{}, std::true_type{}, sa, sb, t);
+          if (t + 1 < nt) step(std::false_type{}, std::true_type{}, sb, sa, t + 1);
+        }
+      } else {
+        for (int t = 0; t + 1 < nt; ++t) {
+          if (t + 2 < nt) wait_vmcnt<LPT>();
+          else wait_vmcnt<0>();
+          __syncthreads();
+          if (t + 3 < nt) issue_tile(t + 3);
+        }
+      }
+    }
+
+    const float total = pair_sum(l_run);
+    if (r >= w.M) return;
+    const float by = !seg.whole ? 1.f : total > 0.f ? 1.f / total : 0.f;
+    const long long at_part = (long long)seg.slot * kTileRows + r - seg.r0;
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int d = db * 32 + 2 * i + 4 * h;
+        const f32x4 x = {o[db][i] * by, o[db][i + 1] * by, o[db][i + 2] * by, o[db][i + 3] * by};
+        if (seg.whole)
+          *reinterpret_cast<uint2*>(static_cast<u16*>(p.O) + at_row + d) = uint2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+        else
+          *reinterpret_cast<f32x4*>(p.part_o + at_part * D + d) = x;
+      }
+    if (h == 0) {
+      if (seg.whole) p.lse[at_lse] = total > 0.f ? (m_run * c2 + log2f(total)) * kLn2 : -INFINITY;
+      else *reinterpret_cast<f32x2*>(p.part_ml + at_part * 2) = f32x2{m_run * c2, total};
+    }
+  });
+}
+
+int launch_tiles(const AttnParams& p, hipStream_t st) {
+  if (p.c.D == 128) paged_tile_kernel<128><<<p.n_wgs, kTileThreads, 0, st>>>(p);
+  else paged_tile_kernel<64><<<p.n_wgs, kTileThreads, 0, st>>>(p);
+  OMNI_LAUNCH_CHECK();
+  return OMNI_OK;
+}
+
+// ------------------------------------------------------------------ items that were split, rows of the padding
+
+// grid: (items, blocks of rows of an item).  A wavefront joins a row: the slots of the item's spans in the order of the units.
+constexpr int kCombineThreads = 256, kCombineRows = 4;
+template <typename T, int D>
+__global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(AttnParams p) {
+  __shared__ Scan scan;
+  const int item = blockIdx.x, wave = threadIdx.x >> 6, lane = lane_id();
+  const PairView w(p, item / p.tiles_per_pair);
+  const int r0 = item % p.tiles_per_pair * p.tm;
+  int first, per;
+  u64 own;
+  Spans sp;
+  u64 at = scan_items<kCombineThreads>(p, scan, first, per, own, sp);
+  if (item >= first && item < first + per) {
+    for (int i = first; i < item; ++i) at += item_units(p, i);
+    scan.at = at;
+  }
+  __syncthreads();
+  const u64 begin = scan.at;
+  const int units = item_units(p, item);
+  int w0 = 0, w1 = 0;
+  if (units) {
+    w0 = sp.owner(begin);
+    w1 = sp.owner(begin + units - 1);
+  }
+  const int full = p.c.G * p.c.n_new;
+  constexpr int E = D / 64;
+  for (int k = 0; k < kCombineRows; ++k) {
+    const int rl = (blockIdx.y * kCombineRows + k) * (kCombineThreads / 64) + wave, r = r0 + rl;
+    if (rl >= p.tm || r >= full) break;
+    if (r < w.M && w0 == w1) continue;                   // one span had all of it and wrote the rows
+    long long at_lse;
+    T* dst = static_cast<T*>(p.O) + out_row(p, w, r, at_lse) + lane * E;
+    float m = -INFINITY, l = 0.f, x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = 0.f;
+    if (r < w.M) {
+      auto slot_of = [&](int v) { return 2 * v + (sp.start(v) >= begin ? 0 : 1); };
+      for (int v = w0; v <= w1; ++v) m = fmaxf(m, p.part_ml[((long long)slot_of(v) * p.tm + rl) * 2]);
+      const float ref = m == -INFINITY ? 0.f : m;
+      for (int v = w0; v <= w1; ++v) {
+        const long long row = (long long)slot_of(v) * p.tm + rl;
+        const f32x2 ml = *reinterpret_cast<const f32x2*>(p.part_ml + row * 2);
+        const float wgt = fast_exp2(ml[0] - ref);
+        l = fmaf(ml[1], wgt, l);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = fmaf(p.part_o[row * D + lane * E + e], wgt, x[e]);
+      }
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) Elem<T>::store(dst + e, x[e] * inv);
+    if (lane == 0) p.lse[at_lse] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  }
+}
+
+// ------------------------------------------------------------------ which kernel, how many workgroups
+
+struct Plan {
+  int tm, unit, n_wgs, min_share;
+  bool logits;                                           // scores of the pass are kept for the weights
+};
+
+Plan make_plan(const Chunk& c, int dtype, int weight_rows) {
+  const int rows = c.G * c.n_new;
+  Plan pl;
+  if (rows <= 32) pl = Plan{32, 128, dtype == OMNI_BF16 ? 768 : 256, 1, false};
+  else pl = dtype == OMNI_BF16 ? Plan{256, 64, 256, 2, false} : Plan{128, 32, 512, 2, false};
+  pl.logits = weight_rows > 0 && dtype == OMNI_BF16 && pl.tm == 32;
+  return pl;
+}
+
+void carve(AttnParams& p, const Plan& pl, int weight_rows, void* ws, size_t* bytes) {
+  Arena a(ws);
+  p.part_o = a.take<float>((size_t)2 * pl.n_wgs * pl.tm * p.c.D);
+  p.part_ml = a.take<float>((size_t)2 * pl.n_wgs * pl.tm * 2);
+  p.logits = pl.logits ? a.take<float>((size_t)p.c.B * p.c.Hkv * cdiv(weight_rows, 32) * p.c.G * p.c.n_new * 32) : nullptr;
+  if (bytes) *bytes = a.used();
 }
 
 }  // namespace
 
-size_t paged_attn_ws(const Chunk& c, int dtype, int weight_rows) { return 256; }
+int launch_combine(const AttnParams& p, int dtype, hipStream_t st) {
+  const int rows = min(p.tm, p.c.G * p.c.n_new);
+  const dim3 grid(p.n_items, cdiv(rows, kCombineRows * (kCombineThreads / 64)));
+  if (dtype == OMNI_BF16) {
+    if (p.c.D == 128) paged_combine_kernel<u16, 128><<<grid, kCombineThreads, 0, st>>>(p);
+    else paged_combine_kernel<u16, 64><<<grid, kCombineThreads, 0, st>>>(p);
+  } else {
+    if (p.c.D == 128) paged_combine_kernel<float, 128><<<grid, kCombineThreads, 0, st>>>(p);
+    else paged_combine_kernel<float, 64><<<grid, kCombineThreads, 0, st>>>(p);
+  }
+  OMNI_LAUNCH_CHECK();
+  return OMNI_OK;
+}
+
+size_t paged_attn_ws(const Chunk& c, int dtype, int weight_rows) {
+  AttnParams p{};
+  p.c = c;
+  size_t bytes;
+  carve(p, make_plan(c, dtype, weight_rows), weight_rows, nullptr, &bytes);
+  return bytes;
+}
 
 int run_paged_attn(const Chunk& c, int dtype, const void* Q, const Pages& pg, const int* row_end, const int* new_cnt, void* O,
                    float* lse, const float* acc_in, float* acc_out, void* ws, hipStream_t st) {
   AttnParams p{};
   p.Q = Q; p.O = O; p.lse = lse; p.pg = pg; p.row_end = row_end; p.new_cnt = new_cnt; p.acc_in = acc_in; p.acc_out = acc_out;
   p.c = c;
-  if (dtype == OMNI_BF16) return c.D == 128 ? launch<u16, 128>(p, st) : launch<u16, 64>(p, st);
-  return c.D == 128 ? launch<float, 128>(p, st) : launch<float, 64>(p, st);
+  const int weight_rows = acc_out ? rows_cap(pg) : 0;
+  const Plan pl = make_plan(c, dtype, weight_rows);
+  carve(p, pl, weight_rows, ws, nullptr);
+  p.tm = pl.tm;
+  p.unit = pl.unit;
+  p.n_wgs = pl.n_wgs;
+  p.min_share = pl.min_share;
+  p.tiles_per_pair = cdiv(c.G * c.n_new, pl.tm);
+  p.n_items = c.B * c.Hkv * p.tiles_per_pair;
+  int rc;
+  if (dtype == OMNI_F32) rc = launch_attn_f32(p, st);
+  else if (pl.tm == 32) rc = launch_stream(p, st);
+  else rc = launch_tiles(p, st);
+  if (rc != OMNI_OK) return rc;
+  rc = launch_combine(p, dtype, st);
+  if (rc != OMNI_OK || !acc_out) return rc;
+  return launch_weights(p, dtype, st);
 }
 
 }  // namespace omni

@@ -85,7 +85,7 @@ def test_chunk_descriptors_that_are_refused(lib, kw, code, needle):
 @pytest.mark.parametrize("kw,code,needle", [
     (dict(K=None), -1, "null"), (dict(V=FAKE + 8), -1, "aligned"), (dict(page_table=None), -1, "null"),
     (dict(page_rows=24), -2, "power of two"), (dict(n_pages=0), -1, ">= 1"), (dict(pages_cap=0), -1, ">= 1"),
-    (dict(n_pages=1 << 27), -2, "2^31"), (dict(pages_cap=1 << 27), -2, "2^31"),
+    (dict(n_pages=1 << 27), -2, "2^31"), (dict(pages_cap=1 << 27), -2, "2^30"),
 ])
 def test_pools_that_are_refused(lib, kw, code, needle):
     for call in (_attn, _append, _evict):
