@@ -24,31 +24,87 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------ few query rows: stream the cache
 
+// A wavefront takes 32 cache rows per trip, K and V straight from the pages into a ring of two LDS stages of its own: while one is
+// worked on the other is on its way, 64 to 128 KB per CU in flight, and no barrier in the loop.  (Loads through registers, three
+// workgroups a CU, kept less in flight: 131k rows of eight sequences took 567 us, KEEP_US now.)  An instruction takes 1024 bytes, whole
+// rows of one page; the pieces of a row change places as in the tile kernel below.  Blocks that are not whole go through registers.
 constexpr int kStreamWaves = 4, kStreamThreads = kStreamWaves * 64, kStreamRows = 32;
 
+// where the 16-byte pieces of row r of a tile lie: piece c at c ^ swz(r)
+template <int D>
+__device__ __forceinline__ int swz_k(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
+template <int D>
+__device__ __forceinline__ int swz_v(int row) { return D == 128 ? (row & 3) << 2 : (row & 2) << 1; }
+
 template <int D, bool LOGITS>
-__global__ __launch_bounds__(kStreamThreads, 3) void paged_stream_kernel(AttnParams p) {
-  constexpr int CPR = D / 8, RPI = 64 / CPR, NVL = 32 / RPI, NB = D / 32;
-  constexpr int VP = D * 2 + 16;                         // bytes between rows of a V tile and of the queries
+__global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnParams p) {
+  constexpr int RB = D * 2, CPR = D / 8, RPI = 1024 / RB, NB = D / 32, KS = D / 16;
+  constexpr int kKBytes = 32 * RB, kStageBytes = 2 * kKBytes, LPH = kKBytes / 1024, LPT = 2 * LPH;
+  constexpr int QP = RB + 16;                            // bytes between the queries
   constexpr int OP = 36;                                 // floats between the rows of the merge buffer (32 of the D elements at a time)
-  __shared__ __attribute__((aligned(16))) unsigned char sV[kStreamWaves * 32 * VP], sQ[32 * VP];
+  __shared__ __attribute__((aligned(1024))) unsigned char ring[kStreamWaves * 2 * kStageBytes];
+  __shared__ __attribute__((aligned(16))) unsigned char sQ[32 * QP];
   __shared__ float sM[kStreamWaves][32], sL[kStreamWaves][32];
   __shared__ Scan scan;
-  static_assert(kStreamWaves * 32 * OP * 4 <= (int)sizeof(sV), "the merge buffer takes the V tiles' place");
+  static_assert(kStreamWaves * 32 * OP * 4 <= (int)sizeof(ring), "the merge buffer takes the ring's place");
   const Chunk& c = p.c;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id(), n = lane & 31, h = lane >> 5;
   const float c2 = c.scale * kLog2e;
-  unsigned char* tile = sV + wave * 32 * VP;
-  // transposing reads: a lane supplies four neighbours of one row and gets four rows of one column, in the order in which the
-  // accumulators hold the weights
+  const unsigned own_ring = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)ring + wave * 2 * kStageBytes;
+  unsigned char* own_bytes = ring + wave * 2 * kStageBytes;
+  const unsigned char* Kpool = static_cast<const unsigned char*>(p.pg.K);
+  const unsigned char* Vpool = static_cast<const unsigned char*>(p.pg.V);
+  const int in_row = lane / CPR, slot = lane % CPR;
+  unsigned src_k[16 / RPI > 1 ? 4 : 1];                  // the K swizzle goes through 16 rows: 16 / RPI patterns
+  constexpr int NP = 16 / RPI;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) src_k[i] = in_row * RB + ((slot ^ swz_k<D>(i * RPI + in_row)) * 16);
+  const unsigned src_v = in_row * RB + ((slot ^ swz_v<D>(in_row)) * 16);
+  const unsigned frag_k = n * RB + ((h ^ swz_k<D>(n)) * 16);
+  const unsigned frag_v = kKBytes + (4 * h + (n & 15) / 4) * RB + ((swz_v<D>((n & 15) / 4) + (n >> 4) * 2) * 16) + (n & 3) * 8;
   typedef __attribute__((address_space(3))) s16x4* lds_quads;
-  const lds_quads vcol = (lds_quads)(tile + (4 * h + (n & 15) / 4) * VP + (n & 16) * 2 + (n & 3) * 8);
-  const unsigned char* qlane = sQ + n * VP + h * 16;
-  const u16* Kp = static_cast<const u16*>(p.pg.K);
-  const u16* Vp = static_cast<const u16*>(p.pg.V);
+  typedef __attribute__((address_space(3))) bf16x8* lds_eights;
+  const unsigned char* qlane = sQ + n * QP + h * 16;
 
   for_segments<kStreamThreads>(p, scan, blockIdx.x, [&](const Segment& seg) {
     const PairView w(p, seg.pair);
+    const int keys = w.visible(p, (w.M - 1) / c.G);
+    const int first = seg.u0 * kStreamWaves + wave, last = min(seg.u1 * kStreamWaves, cdiv(keys, 32));
+    const int* table = p.pg.table + (long long)seg.pair * p.pg.pages_cap;
+    const int page_mask = (1 << p.pg.shift) - 1;
+    // pool rows of a block's two halves of 16 rows (each inside one page), -1: not there
+    auto half_row = [&](int block, int half) {
+      const int j = block * 32 + half * 16;
+      if (block >= last || j >= w.end) return -1;
+      const int page = table[j >> p.pg.shift];
+      return (unsigned)page < (unsigned)p.pg.n_pages ? (page << p.pg.shift) + (j & page_mask) : -1;
+    };
+    auto issue = [&](int block, int stage, int row_a, int row_b) {
+      const unsigned dst = own_ring + stage * kStageBytes;
+      if (row_a >= 0 && row_b >= 0 && block * 32 + 32 <= w.end) {
+#pragma unroll
+        for (int i = 0; i < LPH; ++i) {
+          const long long row = (long long)(i * RPI < 16 ? row_a : row_b) + i * RPI % 16;
+          gload_lds16(Kpool + row * RB, src_k[i % NP], dst + i * 1024);
+          gload_lds16(Vpool + row * RB, src_v, dst + kKBytes + i * 1024);
+        }
+      } else {                                           // zeros for what is not there; these loads end here
+#pragma unroll
+        for (int i = 0; i < LPH; ++i) {
+          const int r = i * RPI + in_row, from = r < 16 ? row_a : row_b;
+          u32x4 k = {0u, 0u, 0u, 0u}, v = k;
+          if (from >= 0 && block * 32 + r < w.end) {
+            const long long at = ((long long)from + r % 16) * RB + slot * 16;
+            k = *reinterpret_cast<const u32x4*>(Kpool + at);
+            v = *reinterpret_cast<const u32x4*>(Vpool + at);
+          }
+          unsigned char* to = own_bytes + stage * kStageBytes + r * RB;
+          *reinterpret_cast<u32x4*>(to + (slot ^ swz_k<D>(r)) * 16) = k;
+          *reinterpret_cast<u32x4*>(to + kKBytes + (slot ^ swz_v<D>(r)) * 16) = v;
+        }
+      }
+    };
+    int row_a = half_row(first, 0), row_b = half_row(first, 1);
     __syncthreads();                                     // the last segment's queries and merge buffer are done with
     for (int i = threadIdx.x; i < 32 * CPR; i += kStreamThreads) {
       const int r = i / CPR;
@@ -57,50 +113,43 @@ __global__ __launch_bounds__(kStreamThreads, 3) void paged_stream_kernel(AttnPar
         long long at_lse;
         raw = *reinterpret_cast<const u32x4*>(static_cast<const u16*>(p.Q) + out_row(p, w, r, at_lse) + i % CPR * 8);
       }
-      *reinterpret_cast<u32x4*>(sQ + r * VP + i % CPR * 16) = raw;
+      *reinterpret_cast<u32x4*>(sQ + r * QP + i % CPR * 16) = raw;
     }
+    wait_vmcnt<0>();                                     // nothing older is counted below
+    if (first < last) issue(first, 0, row_a, row_b);
+    int next_a = half_row(first + kStreamWaves, 0), next_b = half_row(first + kStreamWaves, 1);
     const int vis = n < w.M ? w.visible(p, n / c.G) : 0;
-    const int keys = w.visible(p, (w.M - 1) / c.G);
     f32x16 o[NB];
 #pragma unroll
     for (int db = 0; db < NB; ++db)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
     float m = -INFINITY, l = 0.f;
-    const int first = seg.u0 * kStreamWaves + wave, last = min(seg.u1 * kStreamWaves, cdiv(keys, 32));
-    auto row_of = [&](int block) {
-      const int j = block * 32 + n;
-      return block < last && j < w.end ? pool_row(p.pg, w.pair, j) : -1;
-    };
-    int row = row_of(first);
     __syncthreads();
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qlane + ks * 32);
+    int stage = 0;
     for (int block = first; block < last; block += kStreamWaves) {
-      bf16x8 kf[D / 16];
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        u32x4 raw = {0u, 0u, 0u, 0u};
-        if (row >= 0) raw = *reinterpret_cast<const u32x4*>(Kp + (long long)row * D + ks * 16 + h * 8);
-        kf[ks] = __builtin_bit_cast(bf16x8, raw);
+      const unsigned there = ((row_a >= 0 ? 0xffffu : 0u) | (row_b >= 0 ? 0xffff0000u : 0u)) >> (4 * h);
+      row_a = next_a;
+      row_b = next_b;
+      if (block + kStreamWaves < last) {
+        issue(block + kStreamWaves, stage ^ 1, row_a, row_b);
+        next_a = half_row(block + 2 * kStreamWaves, 0);
+        next_b = half_row(block + 2 * kStreamWaves, 1);
+        wait_vmcnt<LPT>();
+      } else {
+        wait_vmcnt<0>();
       }
-      u32x4 vraw[NVL];
-#pragma unroll
-      for (int j = 0; j < NVL; ++j) {
-        const int vr = __shfl(row, j * RPI + lane / CPR, 64);
-        vraw[j] = u32x4{0u, 0u, 0u, 0u};
-        if (vr >= 0) vraw[j] = *reinterpret_cast<const u32x4*>(Vp + (long long)vr * D + (lane % CPR) * 8);
-      }
-      const unsigned there = (unsigned)__ballot(row >= 0) >> (4 * h);
-      row = row_of(block + kStreamWaves);                // a row's address depends on its table entry: fetched a trip ahead
+      const unsigned base = own_ring + stage * kStageBytes;
       f32x16 s;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], *reinterpret_cast<const bf16x8*>(qlane + ks * 32), s, 0, 0, 0);
-#pragma unroll
-      for (int j = 0; j < NVL; ++j)
-        *reinterpret_cast<u32x4*>(tile + (j * RPI + lane / CPR) * VP + (lane % CPR) * 16) = vraw[j];
-      const int rel = vis - block * 32 - 4 * h;          // rows of this block from here on are not seen
+      for (int ks = 0; ks < KS; ++ks)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds_eights)(size_t)((base + frag_k) ^ (ks * 32)), qf[ks], s, 0, 0, 0);
+      const int rel = min(vis, w.end) - block * 32 - 4 * h;   // rows of this block from here on are not seen
       float mx = m;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -136,17 +185,18 @@ __global__ __launch_bounds__(kStreamThreads, 3) void paged_stream_kernel(AttnPar
       union { bf16x8 v[2]; unsigned u[8]; } pf;
 #pragma unroll
       for (int i = 0; i < 16; i += 2) pf.u[i / 2] = pack_bf16x2(s[i], s[i + 1]);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the tile is this wavefront's own: its writes are done
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
         for (int db = 0; db < NB; ++db) {
           union { s16x4 q[2]; bf16x8 v; } vf;
-#pragma unroll
-          for (int half = 0; half < 2; ++half)
-            vf.q[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(vcol + ((16 * s2 + 8 * half) * VP + 64 * db) / 8);
+          const unsigned at = ((base + frag_v) ^ (db * 64)) + s2 * 16 * RB;
+          vf.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quads)(size_t)at);
+          vf.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quads)(size_t)(at + 8 * RB));
           o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf.v[s2], o[db], 0, 0, 0);
         }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // this stage is read: the next trip's copies may overwrite it
+      stage ^= 1;
     }
     // join the wavefronts in their order, 32 elements of the rows at a time
     const float own = pair_sum(l);
@@ -173,19 +223,22 @@ __global__ __launch_bounds__(kStreamThreads, 3) void paged_stream_kernel(AttnPar
       }
     }
     const float by = seg.whole ? mine * inv : mine;
-    float* sO = reinterpret_cast<float*>(sV);
+    float* sO = reinterpret_cast<float*>(ring);          // a buffer per group of 32 elements where the ring has the space
+    constexpr int kGroup = kStreamWaves * 32 * OP;
+    static_assert(NB * kGroup * 4 <= (int)sizeof(ring), "");
 #pragma unroll
-    for (int db = 0; db < NB; ++db) {
-      __syncthreads();                                   // tiles, or the elements before, are done with
+    for (int db = 0; db < NB; ++db)
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<f32x4*>(sO + (wave * 32 + n) * OP + 2 * i + 4 * h) = f32x4{o[db][i] * by, o[db][i + 1] * by, o[db][i + 2] * by, o[db][i + 3] * by};
-      __syncthreads();
+        *reinterpret_cast<f32x4*>(sO + db * kGroup + (wave * 32 + n) * OP + 2 * i + 4 * h) = f32x4{o[db][i] * by, o[db][i + 1] * by, o[db][i + 2] * by, o[db][i + 3] * by};
+    __syncthreads();
+#pragma unroll
+    for (int db = 0; db < NB; ++db) {
       const int r = threadIdx.x / 8, d = threadIdx.x % 8 * 4;
       if (r < w.M) {
-        f32x4 x = *reinterpret_cast<const f32x4*>(sO + r * OP + d);
+        f32x4 x = *reinterpret_cast<const f32x4*>(sO + db * kGroup + r * OP + d);
 #pragma unroll
-        for (int v = 1; v < kStreamWaves; ++v) x += *reinterpret_cast<const f32x4*>(sO + (v * 32 + r) * OP + d);
+        for (int v = 1; v < kStreamWaves; ++v) x += *reinterpret_cast<const f32x4*>(sO + db * kGroup + (v * 32 + r) * OP + d);
         if (seg.whole) {
           long long at_lse;
           u16* dst = static_cast<u16*>(p.O) + out_row(p, w, r, at_lse) + db * 32 + d;
@@ -243,17 +296,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
   const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem;
   const unsigned char* Kpool = static_cast<const unsigned char*>(p.pg.K);
   const unsigned char* Vpool = static_cast<const unsigned char*>(p.pg.V);
-  auto swz_k = [](int row) { return D == 128 ? row & 15 : row >> 1 & 7; };
-  auto swz_v = [](int row) { return D == 128 ? (row & 3) << 2 : (row & 2) << 1; };
 
   // a lane's source inside the rows that an instruction takes (the instruction's first row is a multiple of RPI = 4 or 8; for K
   // the row's low bits beyond that are the wavefront's)
   const int in_row = lane / CPR, slot = lane % CPR;
-  const unsigned src_k = in_row * RB + ((slot ^ swz_k(wave * RPI + in_row)) * 16);
-  const unsigned src_v = in_row * RB + ((slot ^ swz_v(in_row)) * 16);
+  const unsigned src_k = in_row * RB + ((slot ^ swz_k<D>(wave * RPI + in_row)) * 16);
+  const unsigned src_v = in_row * RB + ((slot ^ swz_v<D>(in_row)) * 16);
   // a lane's fragments: K row ln (+ 32), piece 2 ks + h; V rows 4 h + .. (+ 8, 16 t), 16 bytes of a column group
-  const unsigned frag_k = ln * RB + ((h ^ swz_k(ln)) * 16);
-  const unsigned frag_v = kKBytes + (4 * h + (ln & 15) / 4) * RB + ((swz_v((ln & 15) / 4) + (ln >> 4) * 2) * 16) + (ln & 3) * 8;
+  const unsigned frag_k = ln * RB + ((h ^ swz_k<D>(ln)) * 16);
+  const unsigned frag_v = kKBytes + (4 * h + (ln & 15) / 4) * RB + ((swz_v<D>((ln & 15) / 4) + (ln >> 4) * 2) * 16) + (ln & 3) * 8;
   typedef __attribute__((address_space(3))) s16x4* lds_quads;
   typedef __attribute__((address_space(3))) bf16x8* lds_eights;
   const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -323,8 +374,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
             k = *reinterpret_cast<const u32x4*>(Kpool + src);
             v = *reinterpret_cast<const u32x4*>(Vpool + src);
           }
-          *reinterpret_cast<u32x4*>(dst + row * RB + (piece ^ swz_k(row)) * 16) = k;
-          *reinterpret_cast<u32x4*>(dst + kKBytes + row * RB + (piece ^ swz_v(row)) * 16) = v;
+          *reinterpret_cast<u32x4*>(dst + row * RB + (piece ^ swz_k<D>(row)) * 16) = k;
+          *reinterpret_cast<u32x4*>(dst + kKBytes + row * RB + (piece ^ swz_v<D>(row)) * 16) = v;
         }
       };
       auto issue_tile = [&](int t) {
@@ -533,12 +584,16 @@ int launch_tiles(const AttnParams& p, hipStream_t st) {
 
 // ------------------------------------------------------------------ items that were split, rows of the padding
 
-// grid: (items, blocks of rows of an item).  A wavefront joins a row: the slots of the item's spans in the order of the units.
-constexpr int kCombineThreads = 256, kCombineRows = 4;
-template <typename T, int D>
+// grid: (items, blocks of rows of an item).  WPR wavefronts join a row: the slots of the item's spans in the order of the units
+// (of every WPR-th wavefront its own, then the wavefronts in their order).
+constexpr int kCombineThreads = 256;
+template <typename T, int D, int WPR>
 __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(AttnParams p) {
+  constexpr int kWaves = kCombineThreads / 64, kRowsAtOnce = kWaves / WPR, E = D / 64;
+  constexpr int kRowsPerWg = WPR == 1 ? 16 : 1;
   __shared__ Scan scan;
-  const int item = blockIdx.x, wave = threadIdx.x >> 6, lane = lane_id();
+  __shared__ float sX[WPR == 1 ? 1 : WPR][D], sMl[WPR == 1 ? 1 : WPR][2];
+  const int item = blockIdx.x, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id();
   const PairView w(p, item / p.tiles_per_pair);
   const int r0 = item % p.tiles_per_pair * p.tm;
   int first, per;
@@ -552,16 +607,16 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(AttnPara
   __syncthreads();
   const u64 begin = scan.at;
   const int units = item_units(p, item);
-  int w0 = 0, w1 = 0;
+  int w0 = 0, w1 = 0, shared_first = 0;
   if (units) {
-    w0 = sp.owner(begin);
-    w1 = sp.owner(begin + units - 1);
+    w0 = __builtin_amdgcn_readfirstlane(sp.owner(begin));
+    w1 = __builtin_amdgcn_readfirstlane(sp.owner(begin + units - 1));
+    shared_first = sp.start(w0) < begin ? 1 : 0;        // the first span's item was another one: this one lies in its second slot
   }
   const int full = p.c.G * p.c.n_new;
-  constexpr int E = D / 64;
-  for (int k = 0; k < kCombineRows; ++k) {
-    const int rl = (blockIdx.y * kCombineRows + k) * (kCombineThreads / 64) + wave, r = r0 + rl;
-    if (rl >= p.tm || r >= full) break;
+  for (int k = 0; k < kRowsPerWg; k += kRowsAtOnce) {
+    const int rl = blockIdx.y * kRowsPerWg + k + wave / WPR, r = r0 + rl;
+    if (rl >= p.tm || r >= full) break;                 // WPR > 1: all wavefronts alike
     if (r < w.M && w0 == w1) continue;                   // one span had all of it and wrote the rows
     long long at_lse;
     T* dst = static_cast<T*>(p.O) + out_row(p, w, r, at_lse) + lane * E;
@@ -569,16 +624,32 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(AttnPara
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = 0.f;
     if (r < w.M) {
-      auto slot_of = [&](int v) { return 2 * v + (sp.start(v) >= begin ? 0 : 1); };
-      for (int v = w0; v <= w1; ++v) m = fmaxf(m, p.part_ml[((long long)slot_of(v) * p.tm + rl) * 2]);
+      auto slot_row = [&](int v) { return (long long)(2 * v + (v == w0 ? shared_first : 0)) * p.tm + rl; };
+      for (int v = w0 + lane; v <= w1; v += 64) m = fmaxf(m, p.part_ml[slot_row(v) * 2]);
+      m = wave_max(m);
       const float ref = m == -INFINITY ? 0.f : m;
-      for (int v = w0; v <= w1; ++v) {
-        const long long row = (long long)slot_of(v) * p.tm + rl;
+      const int part = wave % WPR;
+#pragma unroll 8
+      for (int v = w0 + part; v <= w1; v += WPR) {
+        const long long row = slot_row(v);
         const f32x2 ml = *reinterpret_cast<const f32x2*>(p.part_ml + row * 2);
         const float wgt = fast_exp2(ml[0] - ref);
         l = fmaf(ml[1], wgt, l);
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = fmaf(p.part_o[row * D + lane * E + e], wgt, x[e]);
+      }
+    }
+    if constexpr (WPR > 1) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) sX[wave][lane * E + e] = x[e];
+      if (lane == 0) sMl[wave][0] = l;
+      __syncthreads();
+      if (wave != 0) return;                             // a workgroup has one row
+#pragma unroll
+      for (int v = 1; v < WPR; ++v) {
+        l += sMl[v][0];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] += sX[v][lane * E + e];
       }
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -598,17 +669,19 @@ struct Plan {
 Plan make_plan(const Chunk& c, int dtype, int weight_rows) {
   const int rows = c.G * c.n_new;
   Plan pl;
-  if (rows <= 32) pl = Plan{32, 128, dtype == OMNI_BF16 ? 768 : 256, 1, false};
+  if (rows <= 32) pl = Plan{32, 128, dtype == OMNI_BF16 && c.D == 64 ? 512 : 256, 1, false};
   else pl = dtype == OMNI_BF16 ? Plan{256, 64, 256, 2, false} : Plan{128, 32, 512, 2, false};
   pl.logits = weight_rows > 0 && dtype == OMNI_BF16 && pl.tm == 32;
   return pl;
 }
 
-void carve(AttnParams& p, const Plan& pl, int weight_rows, void* ws, size_t* bytes) {
+void carve(AttnParams& p, const Plan& pl, int dtype, int weight_rows, void* ws, size_t* bytes) {
   Arena a(ws);
   p.part_o = a.take<float>((size_t)2 * pl.n_wgs * pl.tm * p.c.D);
   p.part_ml = a.take<float>((size_t)2 * pl.n_wgs * pl.tm * 2);
   p.logits = pl.logits ? a.take<float>((size_t)p.c.B * p.c.Hkv * cdiv(weight_rows, 32) * p.c.G * p.c.n_new * 32) : nullptr;
+  p.w_splits = weight_rows > 0 && !pl.logits ? weight_splits(p.c, dtype, weight_rows) : 1;
+  p.w_part = p.w_splits > 1 ? a.take<float>((size_t)p.w_splits * p.c.B * p.c.Hkv * weight_rows) : nullptr;
   if (bytes) *bytes = a.used();
 }
 
@@ -616,14 +689,17 @@ void carve(AttnParams& p, const Plan& pl, int weight_rows, void* ws, size_t* byt
 
 int launch_combine(const AttnParams& p, int dtype, hipStream_t st) {
   const int rows = min(p.tm, p.c.G * p.c.n_new);
-  const dim3 grid(p.n_items, cdiv(rows, kCombineRows * (kCombineThreads / 64)));
+#define OMNI_COMBINE(T, D)                                                                                                       \
+  (p.tm == 32 ? paged_combine_kernel<T, D, 4><<<dim3(p.n_items, rows), kCombineThreads, 0, st>>>(p)                              \
+              : paged_combine_kernel<T, D, 1><<<dim3(p.n_items, cdiv(rows, 16)), kCombineThreads, 0, st>>>(p))
   if (dtype == OMNI_BF16) {
-    if (p.c.D == 128) paged_combine_kernel<u16, 128><<<grid, kCombineThreads, 0, st>>>(p);
-    else paged_combine_kernel<u16, 64><<<grid, kCombineThreads, 0, st>>>(p);
+    if (p.c.D == 128) OMNI_COMBINE(u16, 128);
+    else OMNI_COMBINE(u16, 64);
   } else {
-    if (p.c.D == 128) paged_combine_kernel<float, 128><<<grid, kCombineThreads, 0, st>>>(p);
-    else paged_combine_kernel<float, 64><<<grid, kCombineThreads, 0, st>>>(p);
+    if (p.c.D == 128) OMNI_COMBINE(float, 128);
+    else OMNI_COMBINE(float, 64);
   }
+#undef OMNI_COMBINE
   OMNI_LAUNCH_CHECK();
   return OMNI_OK;
 }
@@ -632,7 +708,7 @@ size_t paged_attn_ws(const Chunk& c, int dtype, int weight_rows) {
   AttnParams p{};
   p.c = c;
   size_t bytes;
-  carve(p, make_plan(c, dtype, weight_rows), weight_rows, nullptr, &bytes);
+  carve(p, make_plan(c, dtype, weight_rows), dtype, weight_rows, nullptr, &bytes);
   return bytes;
 }
 
@@ -643,7 +719,7 @@ int run_paged_attn(const Chunk& c, int dtype, const void* Q, const Pages& pg, co
   p.c = c;
   const int weight_rows = acc_out ? rows_cap(pg) : 0;
   const Plan pl = make_plan(c, dtype, weight_rows);
-  carve(p, pl, weight_rows, ws, nullptr);
+  carve(p, pl, dtype, weight_rows, ws, nullptr);
   p.tm = pl.tm;
   p.unit = pl.unit;
   p.n_wgs = pl.n_wgs;

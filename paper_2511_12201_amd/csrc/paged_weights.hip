@@ -5,20 +5,29 @@ namespace omni {
 
 namespace {
 
-template <typename T>
-__device__ __forceinline__ float to_f32(T x);
-template <>
-__device__ __forceinline__ float to_f32<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ float to_f32<u16>(u16 x) { return bf16_bits_to_f32(x); }
-
 constexpr int kWaves = 4, kThreads = kWaves * 64, kRows = kWaves * 32;
 
-// Weights from the finished log-sum-exps: a wavefront owns 32 cache rows, all query rows of the pair pass by.
-// grid: (blocks of kRows cache rows, pairs)
-template <typename T, int D>
+// Where the weights of a block of cache rows go: straight to acc_out, or, where the query rows are split, to a plane of their
+// own, and paged_weights_sum_kernel adds the planes in their order.
+__device__ __forceinline__ void put_weight(const AttnParams& p, const PairView& w, int j, float v) {
+  const long long at = (long long)w.pair * rows_cap(p.pg) + j;
+  if (p.w_splits > 1) p.w_part[(long long)blockIdx.z * p.c.B * p.c.Hkv * rows_cap(p.pg) + at] = v;
+  else p.acc_out[at] = (p.acc_in ? p.acc_in[at] : 0.f) + v;
+}
+// The tiles of `rows` query rows that this workgroup goes through: those whose last token sees cache row j0, its share of them.
+__device__ __forceinline__ void tile_range(const AttnParams& p, const PairView& w, int j0, int rows, int& begin, int& end) {
+  const int t_first = p.c.causal ? max(0, j0 - (w.end - w.cnt)) : 0;
+  const int first = (int)min((long long)t_first * p.c.G, (long long)w.M) / rows, n = cdiv(w.M, rows) - first;
+  begin = first + (int)((long long)n * blockIdx.z / p.w_splits);
+  end = first + (int)((long long)n * (blockIdx.z + 1) / p.w_splits);
+}
+
+// fp32.  Weights from the finished log-sum-exps: a wavefront owns 32 cache rows, the query rows pass by.
+// grid: (blocks of kRows cache rows, pairs, splits of the query rows)
+template <int D>
 __global__ __launch_bounds__(kThreads) void paged_weights_f32_kernel(AttnParams p) {
-  __shared__ float sQ[32 * (D + 4)], sL[32];
+  __shared__ __attribute__((aligned(16))) float sQ[32 * (D + 4)];
+  __shared__ float sL[32];
   __shared__ int sVis[32];
   const Chunk& c = p.c;
   const PairView w(p, blockIdx.y);
@@ -31,32 +40,40 @@ __global__ __launch_bounds__(kThreads) void paged_weights_f32_kernel(AttnParams 
 #pragma unroll
   for (int e = 0; e < D / 2; ++e) k[e] = 0.f;
   if (row >= 0) {
-    const T* src = static_cast<const T*>(p.pg.K) + (long long)row * D + h * (D / 2);
+    const float* src = static_cast<const float*>(p.pg.K) + (long long)row * D + h * (D / 2);
 #pragma unroll
-    for (int e = 0; e < D / 2; ++e) k[e] = to_f32<T>(src[e]);
+    for (int e = 0; e < D / 2; e += 4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(src + e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) k[e + i] = x[i];
+    }
   }
   const float c2 = c.scale * kLog2e;
   float sum[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-  constexpr int E = Elem<T>::kPer16B, CPR = D / E;
-  for (int r0 = 0; r0 < w.M; r0 += 32) {
+  constexpr int CPR = D / 4;
+  int t0, t1;
+  tile_range(p, w, blockIdx.x * kRows, 32, t0, t1);
+  for (int r0 = t0 * 32; r0 < t1 * 32; r0 += 32) {
     __syncthreads();
     for (int i = threadIdx.x; i < 32 * CPR; i += kThreads) {
-      const int r = r0 + i / CPR, cc = i % CPR, t = r / c.G, head = w.g * c.G + r % c.G;
-      u32x4 raw = {0u, 0u, 0u, 0u};
-      if (r < w.M)
-        raw = *reinterpret_cast<const u32x4*>(static_cast<const T*>(p.Q) + w.b * c.qs[0] + head * c.qs[1] + t * c.qs[2] + cc * E);
-      float x[E];
-      unpack16(raw, x, (const T*)nullptr);
-#pragma unroll
-      for (int e = 0; e < E; ++e) sQ[(i / CPR) * (D + 4) + cc * E + e] = x[e];
+      const int r = r0 + i / CPR;
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+      long long at_lse;
+      if (r < w.M) x = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.Q) + out_row(p, w, r, at_lse) + i % CPR * 4);
+      *reinterpret_cast<f32x4*>(sQ + (i / CPR) * (D + 4) + i % CPR * 4) = x;
     }
     if (threadIdx.x < 32) {
-      const int r = r0 + threadIdx.x, t = r / c.G, head = w.g * c.G + r % c.G;
-      const float lse = r < w.M ? p.lse[((long long)w.b * c.Hq + head) * c.n_new + t] : -INFINITY;
+      const int r = r0 + threadIdx.x;
+      float lse = -INFINITY;
+      long long at_lse;
+      if (r < w.M) {
+        out_row(p, w, r, at_lse);
+        lse = p.lse[at_lse];
+      }
       sL[threadIdx.x] = lse * kLog2e;
-      sVis[threadIdx.x] = lse > -INFINITY ? w.visible(p, t) : 0;
+      sVis[threadIdx.x] = lse > -INFINITY ? w.visible(p, r / c.G) : 0;
     }
     __syncthreads();
     f32x16 s;
@@ -82,11 +99,138 @@ __global__ __launch_bounds__(kThreads) void paged_weights_f32_kernel(AttnParams 
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     const int j = j0 + 8 * (i / 4) + 4 * h + i % 4;
-    if (ln == 0 && j < w.end) {
-      const long long at = (long long)w.pair * rows_cap(p.pg) + j;
-      p.acc_out[at] = (p.acc_in ? p.acc_in[at] : 0.f) + v;
+    if (ln == 0 && j < w.end) put_weight(p, w, j, v);
+  }
+}
+
+// bf16, many query rows.  A wavefront keeps 64 cache rows as fragments in registers and its 64 sums per lane-half; tiles of 64 query
+// rows pass through LDS, two buffers, one barrier a tile.  Per 64 x 32 weights a wavefront issues 16 matrix instructions (512 cycles)
+// and 32 times scale, 2^x and sum (768 cycles): the vector ALU bounds it, two wavefronts per SIMD overlap the two.
+constexpr int kBfKeys = 64, kBfRows = kWaves * kBfKeys, kBfQ = 64;
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void paged_weights_bf16_kernel(AttnParams p) {
+  constexpr int RB = D * 2, QP = RB + 16, CPR = D / 8, KS = D / 16, NL = kBfQ * CPR / kThreads;
+  __shared__ __attribute__((aligned(16))) unsigned char sQ[2][kBfQ * QP];
+  __shared__ long long sAt[2][kBfQ];
+  __shared__ float sRef[4][kBfQ];
+  __shared__ int sVis[4][kBfQ];
+  const Chunk& c = p.c;
+  const PairView w(p, blockIdx.y);
+  if ((int)blockIdx.x * kBfRows >= w.end) return;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id(), ln = lane & 31, h = lane >> 5;
+  const int j0 = blockIdx.x * kBfRows + wave * kBfKeys;
+  const u16* Kp = static_cast<const u16*>(p.pg.K);
+  const float c2 = c.scale * kLog2e;
+  bf16x8 kf[2][KS];
+  unsigned there[2];
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb) {
+    const int j = j0 + kb * 32 + ln, row = j < w.end ? pool_row(p.pg, w.pair, j) : -1;
+    there[kb] = (unsigned)__ballot(row >= 0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      u32x4 raw = {0u, 0u, 0u, 0u};
+      if (row >= 0) raw = *reinterpret_cast<const u32x4*>(Kp + (long long)row * D + ks * 16 + h * 8);
+      kf[kb][ks] = __builtin_bit_cast(bf16x8, raw);
     }
   }
+  const bool all_there = (there[0] & there[1]) == 0xffffffffu;
+  float sum[2][16];
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[kb][i] = 0.f;
+
+  int t0, t1;
+  tile_range(p, w, blockIdx.x * kBfRows, kBfQ, t0, t1);
+  // where the rows of a tile lie and what they see, by its first wavefront, two tiles ahead
+  auto meta = [&](int tile) {
+    if (threadIdx.x < kBfQ) {
+      const int r = tile * kBfQ + threadIdx.x, rc = min(r, w.M - 1);
+      long long at_lse;
+      sAt[tile & 1][threadIdx.x] = out_row(p, w, rc, at_lse);
+      const float lse = r < w.M && tile < t1 ? p.lse[at_lse] : -INFINITY;
+      sRef[tile & 3][threadIdx.x] = lse > -INFINITY ? lse * kLog2e : 0.f;
+      sVis[tile & 3][threadIdx.x] = lse > -INFINITY ? w.visible(p, rc / c.G) : 0;
+    }
+  };
+  u32x4 raw[NL];
+  auto load = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int piece = i * kThreads + threadIdx.x;
+      raw[i] = *reinterpret_cast<const u32x4*>(static_cast<const u16*>(p.Q) + sAt[tile & 1][piece / CPR] + piece % CPR * 8);
+    }
+  };
+  if (t0 < t1) {
+    meta(t0);
+    meta(t0 + 1);
+    __syncthreads();
+    load(t0);
+    __syncthreads();
+  }
+  for (int tile = t0; tile < t1; ++tile) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int piece = i * kThreads + threadIdx.x;
+      *reinterpret_cast<u32x4*>(&sQ[tile & 1][piece / CPR * QP + piece % CPR * 16]) = raw[i];
+    }
+    if (tile + 1 < t1) load(tile + 1);
+    meta(tile + 2);
+    __syncthreads();
+#pragma unroll
+    for (int qb = 0; qb < 2; ++qb) {
+      const unsigned char* q = &sQ[tile & 1][(qb * 32 + ln) * QP + h * 16];
+      f32x16 s[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 qf = *reinterpret_cast<const bf16x8*>(q + ks * 32);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kb][ks], qf, s[kb], 0, 0, 0);
+      }
+      const float ref = sRef[tile & 3][qb * 32 + ln];
+      const int rel = sVis[tile & 3][qb * 32 + ln] - j0;
+      if (all_there && __all(rel >= kBfKeys)) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[kb][i] += fast_exp2(fmaf(s[kb][i], c2, -ref));
+      } else {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = kb * 32 + 8 * (i / 4) + 4 * h + i % 4;
+            if (key < rel && ((there[kb] >> (key & 31)) & 1u)) sum[kb][i] += fast_exp2(fmaf(s[kb][i], c2, -ref));
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float v = sum[kb][i];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+      const int j = j0 + kb * 32 + 8 * (i / 4) + 4 * h + i % 4;
+      if (ln == 0 && j < w.end) put_weight(p, w, j, v);
+    }
+}
+
+// The planes of split query rows.  grid: (blocks of cache rows, pairs)
+__global__ __launch_bounds__(kThreads) void paged_weights_sum_kernel(AttnParams p) {
+  const PairView w(p, blockIdx.y);
+  const int j = blockIdx.x * kThreads + threadIdx.x;
+  if (j >= w.end) return;
+  const long long at = (long long)w.pair * rows_cap(p.pg) + j, plane = (long long)p.c.B * p.c.Hkv * rows_cap(p.pg);
+  float v = 0.f;
+  for (int s = 0; s < p.w_splits; ++s) v += p.w_part[s * plane + at];
+  p.acc_out[at] = (p.acc_in ? p.acc_in[at] : 0.f) + v;
 }
 
 // The same from scores that the pass over the cache has kept (few query rows): a wavefront takes 32 cache rows at a time, two
@@ -126,18 +270,31 @@ __global__ __launch_bounds__(kThreads) void paged_weights_logits_kernel(AttnPara
 
 }  // namespace
 
+// Workgroups enough for the chip: where the cache rows give few, the query rows are split, a tile or more each.
+int weight_splits(const Chunk& c, int dtype, int cap) {
+  const long long blocks = (long long)c.B * c.Hkv * cdiv(cap, dtype == OMNI_BF16 ? kBfRows : kRows);
+  const int tiles = cdiv(c.G * c.n_new, dtype == OMNI_BF16 ? kBfQ : 32);
+  return (int)max(1ll, min(min(512 / blocks, 16ll), (long long)tiles));
+}
+
 int launch_weights(const AttnParams& p, int dtype, hipStream_t st) {
   const int pairs = p.c.B * p.c.Hkv, cap = rows_cap(p.pg);
   if (p.logits) {
     paged_weights_logits_kernel<<<dim3(cdiv(cap, 32 * kLogitBlocks), pairs), kThreads, 0, st>>>(p);
   } else if (dtype == OMNI_BF16) {
-    if (p.c.D == 128) paged_weights_f32_kernel<u16, 128><<<dim3(cdiv(cap, kRows), pairs), kThreads, 0, st>>>(p);
-    else paged_weights_f32_kernel<u16, 64><<<dim3(cdiv(cap, kRows), pairs), kThreads, 0, st>>>(p);
+    const dim3 grid(cdiv(cap, kBfRows), pairs, p.w_splits);
+    if (p.c.D == 128) paged_weights_bf16_kernel<128><<<grid, kThreads, 0, st>>>(p);
+    else paged_weights_bf16_kernel<64><<<grid, kThreads, 0, st>>>(p);
   } else {
-    if (p.c.D == 128) paged_weights_f32_kernel<float, 128><<<dim3(cdiv(cap, kRows), pairs), kThreads, 0, st>>>(p);
-    else paged_weights_f32_kernel<float, 64><<<dim3(cdiv(cap, kRows), pairs), kThreads, 0, st>>>(p);
+    const dim3 grid(cdiv(cap, kRows), pairs, p.w_splits);
+    if (p.c.D == 128) paged_weights_f32_kernel<128><<<grid, kThreads, 0, st>>>(p);
+    else paged_weights_f32_kernel<64><<<grid, kThreads, 0, st>>>(p);
   }
   OMNI_LAUNCH_CHECK();
+  if (p.w_splits > 1) {
+    paged_weights_sum_kernel<<<dim3(cdiv(cap, kThreads), pairs), kThreads, 0, st>>>(p);
+    OMNI_LAUNCH_CHECK();
+  }
   return OMNI_OK;
 }
 
