@@ -242,6 +242,56 @@ def test_attention_over_pages(shape, weights, dtype):
     check_attention(cache, Q, row_end, new_cnt, causal, weights, dtype)
 
 
+LONG = [
+    # heads, D, n_new, page_rows, row_end per sequence, causal: whole tiles, many spans an item, windows of the page table
+    ((14, 2), 128, 1, 64, (9000, 4097), True), ((8, 2), 64, 3, 16, (20011, 64), True), ((4, 1), 128, 16, 32, (3000, 2999), False),
+    ((14, 2), 128, 100, 64, (4000, 1531), True), ((6, 2), 64, 333, 16, (2222, 900), True), ((4, 1), 128, 24, 16, (70001, 33000), True),
+    ((2, 1), 64, 700, 256, (700, 699), True), ((8, 1), 128, 64, 16, (6400, 6401), False), ((32, 1), 64, 9, 32, (5003, 17), True),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shape", LONG, ids=str)
+def test_attention_over_long_caches(shape, dtype):
+    """The same on the GPU in float64, head by head."""
+    heads, D, n, page_rows, ends, causal = shape
+    rng = np.random.default_rng(n)
+    (H, Hkv), B = heads, 2
+    G = H // Hkv
+    cache = Cache(rng, B, Hkv, -(-max(ends) // page_rows) + 1, page_rows, D, dtype)
+    row_end = [[e - 7 * g if e > n + 7 * Hkv else e for g in range(Hkv)] for e in ends]
+    new_cnt = [n, max(1, min(n - 1, ends[1]))]
+    cache.poison(row_end)
+    Q = rand(rng, B, H, n, D, dtype=dtype) * 2
+    acc_in, acc = torch.rand(B, Hkv, cache.cap, device="cuda"), torch.zeros(B, Hkv, cache.cap, device="cuda")
+    desc = ob.make_chunk_desc(Q, n_kv_heads=Hkv, causal=causal)
+    O, lse = ob.omni_paged_attn(desc, Q, cache.pool, ints(row_end), ints(new_cnt), acc_in=acc_in, acc_out=acc)
+    for b, g in itertools.product(range(B), range(Hkv)):
+        end, cnt = row_end[b][g], new_cnt[b]
+        pages = cache.table[b, g, :-(-end // page_rows)].long()
+        k, v = (x[pages].reshape(-1, D)[:end].double() for x in (cache.K, cache.V))
+        weights = torch.zeros(end, dtype=torch.float64, device="cuda")
+        wl, qk, worst = [], [], 0.0
+        for i in range(g * G, (g + 1) * G):
+            q = Q[b, i, :cnt].double()
+            z = q @ k.T * float(np.float32(desc.softmax_scale))
+            hidden = torch.arange(end, device="cuda") >= (end - cnt + 1 + torch.arange(cnt, device="cuda"))[:, None] if causal else \
+                torch.zeros_like(z, dtype=torch.bool)
+            z.masked_fill_(hidden, -torch.inf)
+            l = z.logsumexp(-1)
+            p = torch.exp(z - torch.where(l > -torch.inf, l, 0.0)[:, None])
+            weights += p.sum(0)
+            reach = ((q.abs() @ k.abs().T).masked_fill(hidden, 0).amax(-1) * desc.softmax_scale).cpu().numpy()
+            pool = type("P", (), {"cap": end})
+            eO, el, ew = attend_bars(host(Q[b, i, :cnt]), pool, dtype, 0, host(p @ v), host(l), host(p @ v.abs()), reach, None, None, G, n)
+            within(host(O[b, i, :cnt]), host(p @ v), eO, f"O {b} {i}")
+            within(host(lse[b, i, :cnt]), host(l), el, f"lse {b} {i}")
+            worst = max(worst, (2 * ((D + 2) * U32 * reach + 2.0 ** -21) + 2 * end * U32 + 4 * U32 * np.abs(host(l))).max())
+        bar = (worst + (2.0 ** -8 if dtype is BF16 else 0) + G * n * U32) * host(weights) + 2 * U32 * np.abs(host(acc_in[b, g, :end]) + host(weights))
+        within(host(acc[b, g, :end]), host(acc_in[b, g, :end]) + host(weights), bar, "weights")
+        assert not O[b, :, cnt:].any() and torch.isneginf(lse[b, :, cnt:]).all()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("n", [1, 6, 50])
 def test_empty_sequences_counts_out_of_range_and_chunks_longer_than_their_rows(dtype, n):
@@ -427,6 +477,18 @@ def test_eviction_with_equal_and_odd_weights(rows, budget, kind):
         acc = rng.choice(np.array([np.nan, -np.nan, np.inf, -np.inf, 0.0, -0.0, 1e-40, -1e-40, 3.0, 2.5], dtype=np.float32), acc.shape)
     pos = torch.arange(cache.cap, device="cuda").int().expand(1, 2, -1).contiguous()
     check_eviction(cache, budget, 0, 0, [cache.cap + 1], [[rows, rows - 1]], pos, torch.from_numpy(acc).cuda(), True)
+
+
+@pytest.mark.parametrize("pages,rows,budget", [(256, 16384, 16383), (256, 16000, 4000), (257, 16448, 100), (257, 300, 299), (257, 0, 5),
+                                               (2000, 128000, 32000), (2000, 127999, 127998), (64, 4096, 1), (65, 4097, 4000)])
+@pytest.mark.parametrize("kind", ["weights", "zeros"])
+def test_eviction_of_long_caches(pages, rows, budget, kind):
+    rng = np.random.default_rng(rows)
+    cache = Cache(rng, 2, 1, pages, 64, 64, BF16)
+    acc = np.exp(2.5 * rng.standard_normal((2, 1, cache.cap))).astype(np.float32) if kind == "weights" else np.zeros((2, 1, cache.cap), dtype=np.float32)
+    pos = torch.arange(cache.cap, device="cuda").int().expand(2, 1, -1).contiguous()
+    sink, recent = min(4, budget - 1), min(64, max(0, budget - 5))
+    check_eviction(cache, budget, sink, recent, [rows, rows // 2], [[rows], [rows // 2 + 1]], pos, torch.from_numpy(acc).cuda())
 
 
 def test_eviction_where_more_rows_are_spared_than_fit_and_pages_are_missing():
