@@ -910,14 +910,21 @@ def omni_dense_decode(desc: DecodeDesc, q, Kcache, Vcache, ctx_len, O=None, ws: 
 _DTYPES = {OMNI_BF16: torch.bfloat16, OMNI_F32: torch.float32}
 
 
+# the stream that torch works on, as a number: the public accessor builds an object first (2.5 us of a call's 14)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
 def _run_on(dev: torch.device, fn, *args):
     """fn(*args, stream) on the tensors' device and its current stream."""
     if dev.type != "cuda":
         raise ValueError(f"tensors must be on the GPU, not on {dev}")
     if dev.index == torch.cuda.current_device():
-        return _check(fn(*args, torch.cuda.current_stream().cuda_stream))
-    with torch.cuda.device(dev):
-        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+        rc = fn(*args, _raw_stream(dev.index))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _raw_stream(dev.index))
+    if rc != 0:
+        _check(rc)
 
 
 def _want(name: str, t: torch.Tensor, dtype, shape, dev):
@@ -928,16 +935,18 @@ def _want(name: str, t: torch.Tensor, dtype, shape, dev):
 
 
 def _want_rows(name: str, t: torch.Tensor, dtype, shape, strides, dev):
-    """The same for what is shaped like Q or K: the strides are the descriptor's."""
-    if t.dtype is not dtype or t.shape != shape or t.device != dev or t.stride(3) != 1 or \
-            any(t.shape[k] > 1 and t.stride(k) != strides[k] for k in range(3)):
-        raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)} with strides {tuple(strides)} and 1 on {dev}, got "
-                         f"{t.dtype} {tuple(t.shape)} with {t.stride()} on {t.device}")
+    """The same for what is shaped like Q or K: the strides are the descriptor's (of a dimension of one element, any)."""
+    if t.dtype is dtype and t.shape == shape and t.device == dev:
+        have = t.stride()
+        if have == strides or have[3] == 1 and all(t.shape[k] == 1 or have[k] == strides[k] for k in range(3)):
+            return
+    raise ValueError(f"{name} must be a {dtype} tensor {tuple(shape)} with strides {strides} on {dev}, got "
+                     f"{t.dtype} {tuple(t.shape)} with {t.stride()} on {t.device}")
 
 
 def _like(t: torch.Tensor, strides) -> torch.Tensor:
     """An uninitialised tensor of t's shape and type with the descriptor's strides."""
-    return torch.empty_strided(t.shape, (*strides, 1), dtype=t.dtype, device=t.device)
+    return torch.empty_strided(t.shape, strides, dtype=t.dtype, device=t.device)
 
 
 def _scratch(ws: Workspace | None, call_id: int, desc, param: int, dev):
@@ -958,11 +967,23 @@ def _pool_of(pool: PagePool, dtype, head_dim: int, dev):
     return table.shape[0], table.shape[1], pool.pages_cap * pool.page_rows
 
 
+def _pairs_desc(pool: PagePool) -> ChunkDesc:
+    """The pairs of a pool's table as omni_paged_evict describes them; made once per pool."""
+    d = getattr(pool, "_pairs", None)
+    if d is None:
+        K, _, table = pool._keep
+        d = pool._pairs = ChunkDesc()
+        d.batch, d.n_kv_heads, d.head_dim, d.dtype = *table.shape[:2], K.shape[2], _dtype_code(K)
+        d.n_q_heads, d.n_new, d.causal, d.softmax_scale = d.n_kv_heads, 1, 1, 1.0
+        d.q_stride = d.kv_stride = (C.c_int64 * 3)(d.n_kv_heads * d.head_dim, d.head_dim, d.head_dim)
+    return d
+
+
 def omni_rope(rope: RopeDesc, desc: LayerDesc, Q, K, pos=None, backward: bool = False, Qout=None, Kout=None):
     """Rotary positions of a layer's Q and K, or (backward) of the gradients dQ and dK: (Qout, Kout).  pos [B, N] int32 (None:
     0, 1, ..); the outputs may be the inputs."""
     dev, dt = Q.device, _DTYPES[desc.dtype]
-    qs, ks = list(desc.q_stride), list(desc.kv_stride)
+    qs, ks = (*desc.q_stride, 1), (*desc.kv_stride, 1)
     B, N, D = desc.batch, desc.n_tokens, desc.head_dim
     _want_rows("Q", Q, dt, (B, desc.n_q_heads, N, D), qs, dev)
     _want_rows("K", K, dt, (B, desc.n_kv_heads, N, D), ks, dev)
@@ -987,14 +1008,14 @@ def omni_paged_append(desc: ChunkDesc, rope: RopeDesc | None, Q, K, V, pool: Pag
     and K is stored as it is.  row_pos and acc [B, Hkv, rows_cap] get the new rows' positions and zeros."""
     dev, dt = K.device, _DTYPES[desc.dtype]
     B, Hkv, n, D = desc.batch, desc.n_kv_heads, desc.n_new, desc.head_dim
-    ks = list(desc.kv_stride)
+    ks = (*desc.kv_stride, 1)
     tb, th, cap = _pool_of(pool, dt, D, dev)
     if (tb, th) != (B, Hkv):
         raise ValueError(f"page_table is for {tb} x {th} pairs, the chunk has {B} x {Hkv}")
     _want_rows("K", K, dt, (B, Hkv, n, D), ks, dev)
     _want_rows("V", V, dt, (B, Hkv, n, D), ks, dev)
     if rope is not None:
-        qs = list(desc.q_stride)
+        qs = (*desc.q_stride, 1)
         _want_rows("Q", Q, dt, (B, desc.n_q_heads, n, D), qs, dev)
         if Qout is None:
             Qout = _like(Q, qs)
@@ -1025,7 +1046,7 @@ def omni_paged_attn(desc: ChunkDesc, Q, pool: PagePool, row_end, new_cnt, O=None
     the rows' attention weights of this step; it may be acc_in."""
     dev, dt = Q.device, _DTYPES[desc.dtype]
     B, Hq, Hkv, n, D = desc.batch, desc.n_q_heads, desc.n_kv_heads, desc.n_new, desc.head_dim
-    qs = list(desc.q_stride)
+    qs = (*desc.q_stride, 1)
     tb, th, cap = _pool_of(pool, dt, D, dev)
     if (tb, th) != (B, Hkv):
         raise ValueError(f"page_table is for {tb} x {th} pairs, the chunk has {B} x {Hkv}")
@@ -1075,10 +1096,7 @@ def omni_paged_evict(pool: PagePool, budget: int, n_sink: int, n_recent: int, se
         acc_out = torch.empty_like(acc)
     else:
         _want("acc_out", acc_out, torch.float32, (B, Hkv, cap), dev)
-    d = ChunkDesc()
-    d.batch, d.n_q_heads, d.n_kv_heads, d.head_dim, d.n_new, d.causal, d.dtype = B, Hkv, Hkv, K.shape[-1], 1, 1, _dtype_code(K)
-    d.softmax_scale = 1.0
-    d.q_stride = d.kv_stride = (C.c_int64 * 3)(Hkv * d.head_dim, d.head_dim, d.head_dim)
+    d = _pairs_desc(pool)
     buf = _scratch(ws, CALL_PAGED_EVICT, d, cap, dev)
     _run_on(dev, load_library().omni_paged_evict, C.byref(d), C.byref(pool), budget, n_sink, n_recent, seq_len.data_ptr(),
             row_end.data_ptr(), row_pos.data_ptr(), acc.data_ptr(), row_cnt.data_ptr(), row_pos_out.data_ptr(),

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
   const unsigned char* qlane = sQ + n * QP + h * 16;
 
   for_segments<kStreamThreads>(p, scan, blockIdx.x, [&](const Segment& seg) {
-    const PairView w(p, seg.pair);
+    const PairView w = PairView::uniform(p, seg.pair);
     const int keys = w.visible(p, (w.M - 1) / c.G);
     const int first = seg.u0 * kStreamWaves + wave, last = min(seg.u1 * kStreamWaves, cdiv(keys, 32));
     const int* table = p.pg.table + (long long)seg.pair * p.pg.pages_cap;
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
     auto half_row = [&](int block, int half) {
       const int j = block * 32 + half * 16;
       if (block >= last || j >= w.end) return -1;
-      const int page = table[j >> p.pg.shift];
+      const int page = __builtin_amdgcn_readfirstlane(table[j >> p.pg.shift]);
       return (unsigned)page < (unsigned)p.pg.n_pages ? (page << p.pg.shift) + (j & page_mask) : -1;
     };
     auto issue = [&](int block, int stage, int row_a, int row_b) {
@@ -310,16 +310,18 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
   const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
   for_segments<kTileThreads>(p, scan, blockIdx.x, [&](const Segment& seg) {
-    const PairView w(p, seg.pair);
+    const PairView w = PairView::uniform(p, seg.pair);
     const bool active = seg.r0 + wave * 32 < w.M;        // wave-uniform: the others only copy
-    const int r = seg.r0 + wave * 32 + ln, rc = min(r, w.M - 1);
+    const int rc = min(seg.r0 + wave * 32 + ln, w.M - 1);
     const int qvis = w.visible(p, rc / c.G) - 4 * h;     // compared with rows of a tile that leave out 4 h
     const int seen_by_all = w.visible(p, seg.r0 / c.G);
-    long long at_lse;
-    const long long at_row = out_row(p, w, rc, at_lse);
     bf16x8 qf[KS];
+    {
+      long long at_lse;
+      const u16* q = static_cast<const u16*>(p.Q) + out_row(p, w, rc, at_lse) + h * 8;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(static_cast<const u16*>(p.Q) + at_row + ks * 16 + h * 8);
+      for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
+    }
     // the loads end here: a wait for them inside the loop would wait for the copies in flight, too
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
@@ -553,10 +555,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
       }
     }
 
+    // the row's place formed anew: no register holds it across the loop
+    const int row_out = seg.r0 + wave * 32 + (loop_lane() & 31);
     const float total = pair_sum(l_run);
-    if (r >= w.M) return;
+    if (row_out >= w.M) return;
+    long long at_lse;
+    const long long at_row = out_row(p, w, row_out, at_lse);
     const float by = !seg.whole ? 1.f : total > 0.f ? 1.f / total : 0.f;
-    const long long at_part = (long long)seg.slot * kTileRows + r - seg.r0;
+    const long long at_part = (long long)seg.slot * kTileRows + row_out - seg.r0;
 #pragma unroll
     for (int db = 0; db < NB; ++db)
 #pragma unroll
@@ -590,29 +596,14 @@ constexpr int kCombineThreads = 256;
 template <typename T, int D, int WPR>
 __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(AttnParams p) {
   constexpr int kWaves = kCombineThreads / 64, kRowsAtOnce = kWaves / WPR, E = D / 64;
-  constexpr int kRowsPerWg = WPR == 1 ? 16 : 1;
-  __shared__ Scan scan;
-  __shared__ float sX[WPR == 1 ? 1 : WPR][D], sMl[WPR == 1 ? 1 : WPR][2];
+  constexpr int kRowsPerWg = WPR == 1 ? 4 : 1;
+  __shared__ float sX[WPR == 1 ? 1 : WPR][D], sL[WPR == 1 ? 1 : WPR];
   const int item = blockIdx.x, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id();
   const PairView w(p, item / p.tiles_per_pair);
   const int r0 = item % p.tiles_per_pair * p.tm;
-  int first, per;
-  u64 own;
-  Spans sp;
-  u64 at = scan_items<kCombineThreads>(p, scan, first, per, own, sp);
-  if (item >= first && item < first + per) {
-    for (int i = first; i < item; ++i) at += item_units(p, i);
-    scan.at = at;
-  }
-  __syncthreads();
-  const u64 begin = scan.at;
-  const int units = item_units(p, item);
-  int w0 = 0, w1 = 0, shared_first = 0;
-  if (units) {
-    w0 = __builtin_amdgcn_readfirstlane(sp.owner(begin));
-    w1 = __builtin_amdgcn_readfirstlane(sp.owner(begin + units - 1));
-    shared_first = sp.start(w0) < begin ? 1 : 0;        // the first span's item was another one: this one lies in its second slot
-  }
+  const int4 join = r0 < w.M ? p.joins[item] : int4{0, 0, 0, 0};       // an item without rows has no entry
+  const int w0 = __builtin_amdgcn_readfirstlane(join.x), w1 = __builtin_amdgcn_readfirstlane(join.y);
+  const int slot0 = __builtin_amdgcn_readfirstlane(join.z);
   const int full = p.c.G * p.c.n_new;
   for (int k = 0; k < kRowsPerWg; k += kRowsAtOnce) {
     const int rl = blockIdx.y * kRowsPerWg + k + wave / WPR, r = r0 + rl;
@@ -624,7 +615,7 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(AttnPara
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = 0.f;
     if (r < w.M) {
-      auto slot_row = [&](int v) { return (long long)(2 * v + (v == w0 ? shared_first : 0)) * p.tm + rl; };
+      auto slot_row = [&](int v) { return (long long)(v == w0 ? slot0 : 2 * v) * p.tm + rl; };
       for (int v = w0 + lane; v <= w1; v += 64) m = fmaxf(m, p.part_ml[slot_row(v) * 2]);
       m = wave_max(m);
       const float ref = m == -INFINITY ? 0.f : m;
@@ -642,12 +633,12 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(AttnPara
     if constexpr (WPR > 1) {
 #pragma unroll
       for (int e = 0; e < E; ++e) sX[wave][lane * E + e] = x[e];
-      if (lane == 0) sMl[wave][0] = l;
+      if (lane == 0) sL[wave] = l;
       __syncthreads();
       if (wave != 0) return;                             // a workgroup has one row
 #pragma unroll
       for (int v = 1; v < WPR; ++v) {
-        l += sMl[v][0];
+        l += sL[v];
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] += sX[v][lane * E + e];
       }
@@ -679,6 +670,7 @@ void carve(AttnParams& p, const Plan& pl, int dtype, int weight_rows, void* ws, 
   Arena a(ws);
   p.part_o = a.take<float>((size_t)2 * pl.n_wgs * pl.tm * p.c.D);
   p.part_ml = a.take<float>((size_t)2 * pl.n_wgs * pl.tm * 2);
+  p.joins = a.take<int4>((size_t)p.c.B * p.c.Hkv * cdiv(p.c.G * p.c.n_new, pl.tm));
   p.logits = pl.logits ? a.take<float>((size_t)p.c.B * p.c.Hkv * cdiv(weight_rows, 32) * p.c.G * p.c.n_new * 32) : nullptr;
   p.w_splits = weight_rows > 0 && !pl.logits ? weight_splits(p.c, dtype, weight_rows) : 1;
   p.w_part = p.w_splits > 1 ? a.take<float>((size_t)p.w_splits * p.c.B * p.c.Hkv * weight_rows) : nullptr;
@@ -691,7 +683,7 @@ int launch_combine(const AttnParams& p, int dtype, hipStream_t st) {
   const int rows = min(p.tm, p.c.G * p.c.n_new);
 #define OMNI_COMBINE(T, D)                                                                                                       \
   (p.tm == 32 ? paged_combine_kernel<T, D, 4><<<dim3(p.n_items, rows), kCombineThreads, 0, st>>>(p)                              \
-              : paged_combine_kernel<T, D, 1><<<dim3(p.n_items, cdiv(rows, 16)), kCombineThreads, 0, st>>>(p))
+              : paged_combine_kernel<T, D, 1><<<dim3(p.n_items, cdiv(rows, 4)), kCombineThreads, 0, st>>>(p))
   if (dtype == OMNI_BF16) {
     if (p.c.D == 128) OMNI_COMBINE(u16, 128);
     else OMNI_COMBINE(u16, 64);

@@ -5,7 +5,8 @@
 // there are workgroups: every workgroup does the same amount of work whatever the lengths are, and the lengths stay on the
 // device.  A workgroup that has all units of an item writes its output rows; otherwise it leaves a partial state (maximum, sum,
 // weighted rows) in one of its two slots (its span's first item: slot 2 w, another one: it can only be the last: 2 w + 1), and
-// paged_combine_kernel joins the slots of an item in the order of the units: equal inputs, equal bits.
+// paged_combine_kernel joins the slots of an item in the order of the units: equal inputs, equal bits.  The workgroup that has an
+// item's first unit writes down which spans share it.
 #pragma once
 
 #include "paged.h"
@@ -30,6 +31,7 @@ struct AttnParams {
   float* part_o;                           // [2 n_wgs, tm, D]
   float* part_ml;                          // [2 n_wgs, tm, 2]: maximum (times scale log2 e), sum
   float* logits;                           // [pairs, cap / 32, M of a full chunk, 32] scores times scale log2 e, -inf: not seen
+  int4* joins;                             // [n_items] of items that are split: first span, last span, slot of the first
   int w_splits;                            // parts of the query rows in the pass for the weights
   float* w_part;                           // [w_splits, pairs, cap] if there are several
 };
@@ -43,6 +45,14 @@ struct PairView {
     cnt = clampi(p.new_cnt[b], 0, p.c.n_new);
     end = clampi(p.row_end[pair], 0, rows_cap(p.pg));
     M = cnt * p.c.G;
+  }
+  // the view of a pair that the whole wavefront works on: addresses and bounds made of it stay in scalar registers
+  __device__ static __forceinline__ PairView uniform(const AttnParams& p, int pair) {
+    PairView w(p, pair);
+    w.cnt = __builtin_amdgcn_readfirstlane(w.cnt);
+    w.end = __builtin_amdgcn_readfirstlane(w.end);
+    w.M = __builtin_amdgcn_readfirstlane(w.M);
+    return w;
   }
   __device__ __forceinline__ int visible(const AttnParams& p, int t) const { return p.c.causal ? max(end - cnt + t + 1, 0) : end; }
 };
@@ -128,6 +138,8 @@ __device__ __forceinline__ void for_segments(const AttnParams& p, Scan& s, int w
     seg.u1 = off + take;
     seg.slot = 2 * w + (pos == begin ? 0 : 1);
     seg.whole = off == 0 && take == units;
+    if (off == 0 && threadIdx.x == 0)                    // who joins the item finds its slots here (whole: first span = last)
+      p.joins[item] = int4{w, seg.whole ? w : sp.owner(pos + units - 1), seg.slot, 0};
     f(seg);
     pos += take;
     off = 0;

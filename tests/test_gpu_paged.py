@@ -194,7 +194,7 @@ def check_attention(cache, Q, row_end, new_cnt, causal, weights, dtype, desc=Non
     desc = desc or ob.make_chunk_desc(Q, n_kv_heads=Hkv, causal=causal)
     acc = torch.rand(B, Hkv, cache.cap, device="cuda") if weights else None
     out = torch.full_like(acc, -7.0) if weights else None
-    O = ob._like(Q, list(desc.q_stride)).fill_(float("nan"))
+    O = ob._like(Q, (*desc.q_stride, 1)).fill_(float("nan"))
     lse = torch.full((B, H, n), float("nan"), device="cuda")
     ob.omni_paged_attn(desc, Q, cache.pool, ints(row_end), ints(new_cnt), O=O, lse=lse, acc_in=acc, acc_out=out)
     torch.cuda.synchronize()
