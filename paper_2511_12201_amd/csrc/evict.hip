@@ -21,7 +21,7 @@ namespace {
 constexpr int kSmallRows = 16384, kSmallThreads = 1024;
 constexpr int kFewMoves = 256;                 // moves that the workgroup of a pair makes itself
 constexpr int kBins = 2048;
-constexpr int kChunks = 32, kChunkThreads = 512;
+constexpr int kChunks = 40, kChunkThreads = 512, kChunkRows = 8;     // 38 whole chunks of at most 4096 rows: 155k rows in one round
 
 struct EvictParams {
   Pages pg;
@@ -32,7 +32,8 @@ struct EvictParams {
   float* acc_out;
   int* moves;                    // [pairs]
   int2* list;                    // [pairs, cap / 2] (from, to)
-  int *hist, *cut;               // many rows: [3][pairs, kChunks, kBins]; [pairs, 4] digits found and rows wanted of the last one
+  int *hist, *total, *above;     // many rows: [3][pairs, kChunks, kBins], [2][pairs, kBins], [pairs, kChunks]
+  int* cut;                      // [pairs, 4] digits found and rows wanted of the last one
 };
 
 __device__ __forceinline__ unsigned rank_key(float acc, bool spared) {
@@ -81,32 +82,36 @@ __device__ __forceinline__ void count_key(int* hist, int bin, bool counts) {
   }
 }
 
-// The bin that holds the need-th largest key, and how many of it are wanted; hist in LDS, all threads call it.
+// The bin that holds the need-th largest key, how many of it are wanted, and whether that is all of it; hist in LDS, all threads
+// call it.
+struct Found {
+  int bin, left, all;
+};
 template <int THREADS>
-__device__ __forceinline__ void find_bin(const int* hist, int need, int* wave_sums, int* out, int& bin, int& left) {
-  constexpr int PER = kBins / THREADS;
+__device__ __forceinline__ Found find_bin(const int* hist, int need, int* wave_sums, int* out) {
+  constexpr int PER = kBins / THREADS, kWaves = THREADS / 64;
   int own = 0, h[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     h[i] = hist[kBins - 1 - ((int)threadIdx.x * PER + i)];       // from the largest key down
     own += h[i];
   }
-  const int inc = (int)wave_scan((unsigned)own);
-  if (lane_id() == 63) wave_sums[threadIdx.x >> 6] = inc;
+  const int inc = (int)wave_scan((unsigned)own), wave = threadIdx.x >> 6;
+  if (lane_id() == 63) wave_sums[wave] = inc;
   __syncthreads();
-  int before = inc - own;
-  for (int v = 0; v < (int)(threadIdx.x >> 6); ++v) before += wave_sums[v];
+  const int sums = (int)wave_scan((unsigned)(lane_id() < kWaves ? wave_sums[lane_id()] : 0));
+  int before = inc - own + (wave ? __shfl(sums, wave - 1, 64) : 0);
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     if (before < need && need <= before + h[i]) {
       out[0] = kBins - 1 - ((int)threadIdx.x * PER + i);
       out[1] = need - before;
+      out[2] = need == before + h[i];
     }
     before += h[i];
   }
   __syncthreads();
-  bin = out[0];
-  left = out[1];
+  return Found{out[0], out[1], out[2]};
 }
 
 // K and V of moved rows and what they carry; LANES lanes a row.
@@ -134,10 +139,10 @@ __device__ __forceinline__ void move_rows(const EvictParams& p, const PairRows& 
 // R rows a thread: row k * kSmallThreads + thread.
 template <int R>
 __global__ __launch_bounds__(kSmallThreads) void evict_small_kernel(EvictParams p) {
-  constexpr int kWaves = kSmallThreads / 64, kCells = R * kWaves;        // (k, wavefront) in the order of the rows
-  __shared__ int hist[kBins];
-  __shared__ int sums[kWaves], out[2];
-  __shared__ unsigned cell[kCells], cell_wave[kWaves];
+  constexpr int kWaves = kSmallThreads / 64, kCells = R * kWaves, CPL = kCells / 64;   // cells (k, wavefront) in the order of the rows
+  __shared__ int hist[3][kBins];
+  __shared__ int sums[kWaves], out[3];
+  __shared__ __attribute__((aligned(16))) unsigned cell[2][kCells];
   const int pair = blockIdx.x, tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
   const PairRows w(p, pair);
   unsigned key[R];
@@ -151,66 +156,84 @@ __global__ __launch_bounds__(kSmallThreads) void evict_small_kernel(EvictParams 
   }
   int movers = 0;
   if (w.keep < w.n) {
+    for (int i = tid; i < 3 * kBins; i += kSmallThreads) hist[0][i] = 0;
 #pragma unroll
     for (int k = 0; k < R; ++k) key[k] = w.key(acc[k], pos[k]);
     unsigned cut = 0;
     int need = w.keep;
+    __syncthreads();
     for (int d = 0; d < 3; ++d) {
-      for (int i = tid; i < kBins; i += kSmallThreads) hist[i] = 0;
-      __syncthreads();
 #pragma unroll
       for (int k = 0; k < R; ++k) {
         if (k * kSmallThreads + wave * 64 < w.n)         // wave-uniform
-          count_key(hist, digit_of(key[k], d), k * kSmallThreads + tid < w.n && same_above(key[k], cut, d));
+          count_key(hist[d], digit_of(key[k], d), k * kSmallThreads + tid < w.n && same_above(key[k], cut, d));
       }
       __syncthreads();
-      int bin;
-      find_bin<kSmallThreads>(hist, need, sums, out, bin, need);
-      cut = with_digit(cut, bin, d);
-      __syncthreads();
+      const Found f = find_bin<kSmallThreads>(hist[d], need, sums, out);
+      cut = with_digit(cut, f.bin, d);
+      need = f.left;
+      if (f.all) {                                       // every key from here on stays, whatever its other digits
+        need = 0x7fffffff;
+        break;
+      }
     }
-    // exclusive counts of the cells, in order; a cell holds two counts of 16 bits (a pair has at most 16384 rows)
-    auto scan_cells = [&]() {
-      __syncthreads();
-      unsigned own = tid < kCells ? cell[tid] : 0u;
-      const unsigned inc = wave_scan(own);
-      if (lane == 63) cell_wave[wave] = inc;
-      __syncthreads();
-      unsigned before = inc - own;
-      for (int v = 0; v < wave; ++v) before += cell_wave[v];
-      if (tid < kCells) cell[tid] = before;
-      __syncthreads();
+    // in front of a thread's cell k: the counts of the cells before; 16 bits each for two kinds (a pair has at most 16384 rows)
+    unsigned base[CPL];
+    auto scan_cells = [&](const unsigned* c) {
+      unsigned sum = 0;
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) {
+        base[i] = sum;
+        sum += c[lane * CPL + i];
+      }
+      const unsigned before = wave_scan(sum) - sum;
+#pragma unroll
+      for (int i = 0; i < CPL; ++i) base[i] += before;
+    };
+    auto before_cell = [&](int k) {
+      unsigned v = base[0];                              // cell k * kWaves + wave is piece wave % CPL of lane (k * kWaves + wave) / CPL
+#pragma unroll
+      for (int i = 1; i < CPL; ++i) v = wave % CPL == i ? base[i] : v;
+      return __shfl(v, (k * kWaves + wave) / CPL, 64);
     };
     const unsigned long long below = (1ull << lane) - 1;
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      const unsigned long long b = __ballot(k * kSmallThreads + tid < w.n && key[k] == cut);
-      if (lane == 0) cell[k * kWaves + wave] = __popcll(b);
-    }
-    scan_cells();
     unsigned stay = 0;
+    if (need == 0x7fffffff) {
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-      const int j = k * kSmallThreads + tid;
-      const bool tie = j < w.n && key[k] == cut;
-      const unsigned long long b = __ballot(tie);
-      if (j < w.n && (key[k] > cut || (tie && (int)cell[k * kWaves + wave] + __popcll(b & below) < need))) stay |= 1u << k;
+      for (int k = 0; k < R; ++k)
+        if (k * kSmallThreads + tid < w.n && key[k] >= cut) stay |= 1u << k;
+    } else {
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        const unsigned long long b = __ballot(k * kSmallThreads + tid < w.n && key[k] == cut);
+        if (lane == 0) cell[0][k * kWaves + wave] = __popcll(b);
+      }
+      __syncthreads();
+      scan_cells(cell[0]);
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        const int j = k * kSmallThreads + tid;
+        const bool tie = j < w.n && key[k] == cut;
+        const unsigned long long b = __ballot(tie);
+        const int before = (int)before_cell(k) + __popcll(b & below);
+        if (j < w.n && (key[k] > cut || (tie && before < need))) stay |= 1u << k;
+      }
     }
-    __syncthreads();
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       const int j = k * kSmallThreads + tid;
       const bool s = stay >> k & 1u;
       const unsigned long long bh = __ballot(j < w.keep && !s), bm = __ballot(j >= w.keep && s);
-      if (lane == 0) cell[k * kWaves + wave] = (unsigned)__popcll(bh) | (unsigned)__popcll(bm) << 16;
+      if (lane == 0) cell[1][k * kWaves + wave] = (unsigned)__popcll(bh) | (unsigned)__popcll(bm) << 16;
     }
-    scan_cells();
+    __syncthreads();
+    scan_cells(cell[1]);
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       const int j = k * kSmallThreads + tid;
       const bool s = stay >> k & 1u, hole = j < w.keep && !s, mover = j >= w.keep && s;
       const unsigned long long bh = __ballot(hole), bm = __ballot(mover);
-      const unsigned before = cell[k * kWaves + wave];
+      const unsigned before = before_cell(k);
       if (hole) w.list[(before & 0xffffu) + __popcll(bh & below)].y = j;
       if (mover) w.list[(before >> 16) + __popcll(bm & below)].x = j;
       if (j < w.keep && s) {
@@ -248,61 +271,107 @@ __device__ __forceinline__ void chunk_rows(const PairRows& w, int c, int& begin,
   end = max(begin, end);
 }
 
-// The histogram of a digit added up over the chunks of the pair into LDS.
-__device__ __forceinline__ void sum_hist(const EvictParams& p, int d, int pair, int* hist) {
-  const int* src = p.hist + ((long long)d * gridDim.y + pair) * kChunks * kBins;
+// One entry of `hist` per (digit, pair, chunk, bin), of `total` per (digit 1 or 2, pair, bin), of `above` per (pair, chunk).
+__device__ __forceinline__ int* chunk_hist(const EvictParams& p, int d, int pair, int c) {
+  return p.hist + (((long long)d * gridDim.y + pair) * kChunks + c) * kBins;
+}
+__device__ __forceinline__ int* pair_total(const EvictParams& p, int d, int pair) { return p.total + ((long long)(d - 1) * gridDim.y + pair) * kBins; }
+
+// Digit d of all chunks of the pair into LDS: the chunks' histograms added up (digit 0), or what they have added to the pair's.
+__device__ __forceinline__ void load_total(const EvictParams& p, int d, int pair, int* hist) {
   for (int i = threadIdx.x * 4; i < kBins; i += kChunkThreads * 4) {
     i32x4 s = {0, 0, 0, 0};
+    if (d == 0) {
+      const int* src = chunk_hist(p, 0, pair, 0) + i;
 #pragma unroll 8
-    for (int c = 0; c < kChunks; ++c) s += *reinterpret_cast<const i32x4*>(src + c * kBins + i);
+      for (int c = 0; c < kChunks; ++c) s += *reinterpret_cast<const i32x4*>(src + c * kBins);
+    } else {
+      s = *reinterpret_cast<const i32x4*>(pair_total(p, d, pair) + i);
+    }
     *reinterpret_cast<i32x4*>(hist + i) = s;
   }
   __syncthreads();
 }
 
-// Histogram of digit D among the keys that share the digits found so far.
+// Histogram of digit D among the keys that share the digits found so far.  Digit 0 also clears the pair's totals of the other two.
 template <int D>
 __global__ __launch_bounds__(kChunkThreads) void evict_digit_kernel(EvictParams p) {
+  constexpr int kWaves = kChunkThreads / 64;
   __shared__ __attribute__((aligned(16))) int hist[kBins];
-  __shared__ int sums[kChunkThreads / 64], out[2];
+  __shared__ int sums[kWaves], out[3];
   const int pair = blockIdx.y, tid = threadIdx.x;
   const PairRows w(p, pair);
   if (w.keep == w.n) return;
+  int begin, end;
+  chunk_rows(w, blockIdx.x, begin, end);
+  float acc[kChunkRows];
+  int pos[kChunkRows];
+  auto load = [&](int j0) {
+#pragma unroll
+    for (int k = 0; k < kChunkRows; ++k) {
+      const int j = j0 + k * kChunkThreads + tid;
+      acc[k] = j < end ? w.acc[j] : 0.f;
+      pos[k] = j < end ? w.pos[j] : 0;
+    }
+  };
+  load(begin);                                           // on their way while the digit before is found
   unsigned prefix = 0;
   if constexpr (D > 0) {
-    int need = D == 1 ? w.keep : p.cut[pair * 4 + 1];
+    const int need = D == 1 ? w.keep : p.cut[pair * 4 + 1];
     prefix = D == 1 ? 0u : (unsigned)p.cut[pair * 4];
-    sum_hist(p, D - 1, pair, hist);
-    int bin;
-    find_bin<kChunkThreads>(hist, need, sums, out, bin, need);
-    prefix = with_digit(prefix, bin, D - 1);
+    load_total(p, D - 1, pair, hist);
+    const Found f = find_bin<kChunkThreads>(hist, need, sums, out);
+    prefix = with_digit(prefix, f.bin, D - 1);
     if (blockIdx.x == 0 && tid == 0) {                   // for the next launch; digits of different launches do not meet
       p.cut[pair * 4 + (D == 1 ? 0 : 2)] = (int)prefix;
-      p.cut[pair * 4 + (D == 1 ? 1 : 3)] = need;
+      p.cut[pair * 4 + (D == 1 ? 1 : 3)] = f.left;
     }
+    // keys of this chunk above the bin
+    const int* own = chunk_hist(p, D - 1, pair, blockIdx.x);
+    int n = 0;
+    for (int i = tid; i < kBins; i += kChunkThreads) n += i > f.bin ? own[i] : 0;
+    n = wave_sum(n);
+    if (lane_id() == 0) sums[tid >> 6] = n;
     __syncthreads();
+    if (tid == 0) {
+      n = D == 1 ? 0 : p.above[pair * kChunks + blockIdx.x];
+      for (int v = 0; v < kWaves; ++v) n += sums[v];
+      p.above[pair * kChunks + blockIdx.x] = n;
+    }
+  } else if (blockIdx.x == 0) {
+    for (int i = tid; i < kBins; i += kChunkThreads) pair_total(p, 1, pair)[i] = pair_total(p, 2, pair)[i] = 0;
   }
   for (int i = tid; i < kBins; i += kChunkThreads) hist[i] = 0;
   __syncthreads();
-  int begin, end;
-  chunk_rows(w, blockIdx.x, begin, end);
-  for (int j0 = begin; j0 < end; j0 += kChunkThreads) {
-    const int j = j0 + tid;
-    const unsigned k = j < end ? w.key(w.acc[j], w.pos[j]) : 0u;
-    count_key(hist, digit_of(k, D), j < end && same_above(k, prefix, D));
+  for (int j0 = begin; j0 < end; j0 += kChunkRows * kChunkThreads) {
+    if (j0 != begin) load(j0);
+#pragma unroll
+    for (int k = 0; k < kChunkRows; ++k) {
+      const unsigned key = w.key(acc[k], pos[k]);
+      count_key(hist, digit_of(key, D), j0 + k * kChunkThreads + tid < end && same_above(key, prefix, D));
+    }
   }
   __syncthreads();
-  int* dst = p.hist + (((long long)D * gridDim.y + pair) * kChunks + blockIdx.x) * kBins;
-  for (int i = tid * 4; i < kBins; i += kChunkThreads * 4) *reinterpret_cast<i32x4*>(dst + i) = *reinterpret_cast<const i32x4*>(hist + i);
+  int* dst = chunk_hist(p, D, pair, blockIdx.x);
+  for (int i = tid * 4; i < kBins; i += kChunkThreads * 4) {
+    const i32x4 h = *reinterpret_cast<const i32x4*>(hist + i);
+    *reinterpret_cast<i32x4*>(dst + i) = h;
+    if constexpr (D > 0) {                               // integers: the order of the additions does not matter
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (h[e]) atomicAdd(pair_total(p, D, pair) + i + e, h[e]);
+    }
+  }
 }
 
 // Lists of holes and movers, and what the rows that stay carry.  A chunk's first places follow from the histograms: the rows of
 // a chunk above the cut, and its ties.
 __global__ __launch_bounds__(kChunkThreads) void evict_lists_kernel(EvictParams p) {
-  constexpr int kWaves = kChunkThreads / 64;
+  constexpr int kWaves = kChunkThreads / 64, R = kChunkRows, kRound = R * kChunkThreads;
+  static_assert(R * kWaves == 64, "a lane a cell");
   __shared__ __attribute__((aligned(16))) int hist[kBins];
-  __shared__ int sums[kWaves], out[2], above[kChunks], ties[kChunks], start[3];
-  __shared__ int wave_tie[kWaves], wave_hole[kWaves], wave_move[kWaves];
+  __shared__ int sums[kWaves], out[3], above[kChunks], ties[kChunks], start[3];
+  __shared__ unsigned cell[2][64];
   const int pair = blockIdx.y, tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
   const PairRows w(p, pair);
   int begin, end;
@@ -318,23 +387,35 @@ __global__ __launch_bounds__(kChunkThreads) void evict_lists_kernel(EvictParams 
     }
     return;
   }
-  int need = p.cut[pair * 4 + 3];
-  unsigned cut = (unsigned)p.cut[pair * 4 + 2];
-  sum_hist(p, 2, pair, hist);
-  int bin;
-  find_bin<kChunkThreads>(hist, need, sums, out, bin, need);
-  cut = with_digit(cut, bin, 2);
-  // rows above the cut and ties of every chunk: a wavefront takes every kWaves-th chunk
+  float acc[R];
+  int pos[R];
+  auto load = [&](int j0) {
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const int j = j0 + k * kChunkThreads + tid;
+      acc[k] = j < end ? w.acc[j] : 0.f;
+      pos[k] = j < end ? w.pos[j] : 0;
+    }
+  };
+  load(begin);
+  load_total(p, 2, pair, hist);
+  const Found f = find_bin<kChunkThreads>(hist, p.cut[pair * 4 + 3], sums, out);
+  const unsigned cut = with_digit((unsigned)p.cut[pair * 4 + 2], f.bin, 2);
+  const int need = f.left;
+  // rows above the cut and ties of every chunk: a wavefront takes every kWaves-th chunk (the last digit has 1024 bins)
   for (int c = wave; c < kChunks; c += kWaves) {
+    const int* h = chunk_hist(p, 2, pair, c);
     int n = 0;
-    for (int d = 0; d < 3; ++d) {
-      const int* h = p.hist + (((long long)d * gridDim.y + pair) * kChunks + c) * kBins;
-      for (int i = digit_of(cut, d) + 1 + lane; i < kBins; i += 64) n += h[i];
+#pragma unroll
+    for (int i = lane * 4; i < 1024; i += 256) {
+      const i32x4 x = *reinterpret_cast<const i32x4*>(h + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) n += i + e > f.bin ? x[e] : 0;
     }
     n = wave_sum(n);
     if (lane == 0) {
-      above[c] = n;
-      ties[c] = p.hist[((2ll * gridDim.y + pair) * kChunks + c) * kBins + digit_of(cut, 2)];
+      above[c] = n + p.above[pair * kChunks + c];
+      ties[c] = h[f.bin];
     }
   }
   __syncthreads();
@@ -357,48 +438,49 @@ __global__ __launch_bounds__(kChunkThreads) void evict_lists_kernel(EvictParams 
     }
   }
   __syncthreads();
-  int tie0 = start[0], hole0 = start[1], move0 = start[2];
+  int tie0 = start[0], place0 = begin < w.keep ? start[1] : start[2];
+  const bool front = begin < w.keep;                     // holes in front of the new end, movers behind it
   const unsigned long long below = (1ull << lane) - 1;
-  for (int j0 = begin; j0 < end; j0 += kChunkThreads) {
-    const int j = j0 + tid;
-    const float a = j < end ? w.acc[j] : 0.f;
-    const int q = j < end ? w.pos[j] : 0;
-    const unsigned k = w.key(a, q);
-    const bool tie = j < end && k == cut;
-    const unsigned long long bt = __ballot(tie);
-    if (lane == 0) wave_tie[wave] = __popcll(bt);
-    __syncthreads();
-    int before = tie0 + __popcll(bt & below);
+  for (int j0 = begin; j0 < end; j0 += kRound) {
+    if (j0 != begin) load(j0);
+    unsigned long long tie[R];
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
-      if (v < wave) before += wave_tie[v];
-      tie0 += wave_tie[v];
-    }
-    const bool stays = j < end && (k > cut || (tie && before < need));
-    const bool hole = j < end && j < w.keep && !stays, mover = stays && j >= w.keep;
-    const unsigned long long bh = __ballot(hole), bm = __ballot(mover);
-    if (lane == 0) {
-      wave_hole[wave] = __popcll(bh);
-      wave_move[wave] = __popcll(bm);
+    for (int k = 0; k < R; ++k) {
+      tie[k] = __ballot(j0 + k * kChunkThreads + tid < end && w.key(acc[k], pos[k]) == cut);
+      if (lane == 0) cell[0][k * kWaves + wave] = __popcll(tie[k]);
     }
     __syncthreads();
-    int ih = hole0 + __popcll(bh & below), im = move0 + __popcll(bm & below);
+    unsigned own = cell[0][lane], inc = wave_scan(own);
+    unsigned stay = 0;
+    unsigned long long listed[R];
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
-      if (v < wave) {
-        ih += wave_hole[v];
-        im += wave_move[v];
+    for (int k = 0; k < R; ++k) {
+      const int j = j0 + k * kChunkThreads + tid;
+      const int before = tie0 + (int)__shfl(inc - own, k * kWaves + wave, 64) + __popcll(tie[k] & below);
+      const unsigned key = w.key(acc[k], pos[k]);
+      const bool s = j < end && (key > cut || (key == cut && before < need));
+      if (s) stay |= 1u << k;
+      listed[k] = __ballot(j < end && s != front);
+      if (lane == 0) cell[1][k * kWaves + wave] = __popcll(listed[k]);
+    }
+    tie0 += (int)__shfl(inc, 63, 64);
+    __syncthreads();
+    own = cell[1][lane];
+    inc = wave_scan(own);
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const int j = j0 + k * kChunkThreads + tid;
+      const int at = place0 + (int)__shfl(inc - own, k * kWaves + wave, 64) + __popcll(listed[k] & below);
+      if (listed[k] >> lane & 1ull) {
+        if (front) w.list[at].y = j;
+        else w.list[at].x = j;
       }
-      hole0 += wave_hole[v];
-      move0 += wave_move[v];
+      if (front && (stay >> k & 1u)) {
+        w.pos_out[j] = pos[k];
+        w.acc_out[j] = acc[k];
+      }
     }
-    if (hole) w.list[ih].y = j;
-    if (mover) w.list[im].x = j;
-    if (stays && j < w.keep) {
-      w.pos_out[j] = q;
-      w.acc_out[j] = a;
-    }
-    // the next round's first barrier comes after everyone has read wave_tie; wave_hole and wave_move are written after it
+    place0 += (int)__shfl(inc, 63, 64);
   }
 }
 
@@ -418,6 +500,8 @@ void carve(EvictParams& p, int pairs, int cap, Arena& a) {
   if (cap > kSmallRows) {
     p.cut = a.take<int>((size_t)pairs * 4);
     p.hist = a.take<int>((size_t)3 * pairs * kChunks * kBins);
+    p.total = a.take<int>((size_t)2 * pairs * kBins);
+    p.above = a.take<int>((size_t)pairs * kChunks);
   }
 }
 
@@ -444,6 +528,7 @@ int run_paged_evict(int B, int Hkv, int D, int dtype, const Pages& pg, int budge
   if (cap <= kSmallRows) {
     p.move_here = most <= kFewMoves;
     if (cap <= 4 * kSmallThreads) evict_small_kernel<4><<<pairs, kSmallThreads, 0, st>>>(p);
+    else if (cap <= 8 * kSmallThreads) evict_small_kernel<8><<<pairs, kSmallThreads, 0, st>>>(p);
     else evict_small_kernel<16><<<pairs, kSmallThreads, 0, st>>>(p);
     OMNI_LAUNCH_CHECK();
     if (p.move_here) return OMNI_OK;
