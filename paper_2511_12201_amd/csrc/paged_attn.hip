@@ -672,8 +672,12 @@ void carve(AttnParams& p, const Plan& pl, int dtype, int weight_rows, void* ws, 
   p.part_ml = a.take<float>((size_t)2 * pl.n_wgs * pl.tm * 2);
   p.joins = a.take<int4>((size_t)p.c.B * p.c.Hkv * cdiv(p.c.G * p.c.n_new, pl.tm));
   p.logits = pl.logits ? a.take<float>((size_t)p.c.B * p.c.Hkv * cdiv(weight_rows, 32) * p.c.G * p.c.n_new * 32) : nullptr;
-  p.w_splits = weight_rows > 0 && !pl.logits ? weight_splits(p.c, dtype, weight_rows) : 1;
-  p.w_part = p.w_splits > 1 ? a.take<float>((size_t)p.w_splits * p.c.B * p.c.Hkv * weight_rows) : nullptr;
+  if (weight_rows > 0 && !pl.logits) {
+    const WeightPlan wp = weight_plan(dtype, weight_rows);
+    p.w_blocks = wp.blocks;
+    p.w_joins = a.take<int4>((size_t)p.c.B * p.c.Hkv * wp.blocks);
+    p.w_part = a.take<float>(wp.part_floats);
+  }
   if (bytes) *bytes = a.used();
 }
 

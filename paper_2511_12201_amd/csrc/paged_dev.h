@@ -32,8 +32,9 @@ struct AttnParams {
   float* part_ml;                          // [2 n_wgs, tm, 2]: maximum (times scale log2 e), sum
   float* logits;                           // [pairs, cap / 32, M of a full chunk, 32] scores times scale log2 e, -inf: not seen
   int4* joins;                             // [n_items] of items that are split: first span, last span, slot of the first
-  int w_splits;                            // parts of the query rows in the pass for the weights
-  float* w_part;                           // [w_splits, pairs, cap] if there are several
+  int w_blocks;                            // the pass for the weights: blocks of a pair,
+  int4* w_joins;                           // [pairs, w_blocks] as joins,
+  float* w_part;                           // slots of parts
 };
 
 // Query rows and cache rows of a pair: row r is token r / G, head r % G of the group; how many rows a query row sees.
@@ -159,6 +160,10 @@ int launch_combine(const AttnParams& p, int dtype, hipStream_t st);
 int launch_attn_f32(const AttnParams& p, hipStream_t st);
 // paged_weights.hip
 int launch_weights(const AttnParams& p, int dtype, hipStream_t st);
-int weight_splits(const Chunk& c, int dtype, int cap);
+struct WeightPlan {
+  int n_wgs, blocks;
+  size_t part_floats;
+};
+WeightPlan weight_plan(int dtype, int cap);
 
 }  // namespace omni

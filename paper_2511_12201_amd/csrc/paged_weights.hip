@@ -7,33 +7,124 @@ namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * 64, kRows = kWaves * 32;
 
-// Where the weights of a block of cache rows go: straight to acc_out, or, where the query rows are split, to a plane of their
-// own, and paged_weights_sum_kernel adds the planes in their order.
-__device__ __forceinline__ void put_weight(const AttnParams& p, const PairView& w, int j, float v) {
-  const long long at = (long long)w.pair * rows_cap(p.pg) + j;
-  if (p.w_splits > 1) p.w_part[(long long)blockIdx.z * p.c.B * p.c.Hkv * rows_cap(p.pg) + at] = v;
-  else p.acc_out[at] = (p.acc_in ? p.acc_in[at] : 0.f) + v;
+// Work: a block of `keys` cache rows of a pair with the tiles of `rows` query rows whose last token sees its first row.  As in the
+// attention kernels all (block, tile) units are one line cut into equal spans; a workgroup that has all tiles of a block writes
+// its weights, else it leaves its part in a slot, and paged_weights_join_kernel adds the parts in their order.
+struct PairBlocks {
+  int tiles, whole, blocks, base;        // tiles of the pair; blocks that every token sees from the first row on; all blocks
+  __device__ __forceinline__ PairBlocks(const AttnParams& p, const PairView& w, int keys, int rows) {
+    tiles = cdiv(w.M, rows);
+    blocks = w.M ? cdiv(w.end, keys) : 0;
+    base = p.c.causal ? max(w.end - w.cnt, 0) : w.end;
+    whole = min(blocks, base / keys + 1);
+  }
+  // first tile of a block behind `whole`: token j0 - base is the first one that sees row j0
+  __device__ __forceinline__ int first_tile(const AttnParams& p, int block, int keys, int rows) const {
+    return (int)((long long)max(block * keys - base, 0) * p.c.G / rows);
+  }
+  __device__ __forceinline__ u64 units(const AttnParams& p, int keys, int rows) const {
+    u64 n = (u64)whole * tiles;
+    for (int k = whole; k < blocks; ++k) n += tiles - first_tile(p, k, keys, rows);
+    return n;
+  }
+};
+
+struct WeightSegment {
+  int pair, block, t0, t1, slot;
+  bool whole;
+};
+
+template <int THREADS, typename F>
+__device__ __forceinline__ void for_weight_segments(const AttnParams& p, Scan& s, int keys, int rows, F f) {
+  const int pairs = p.c.B * p.c.Hkv, per = cdiv(pairs, THREADS), w = blockIdx.x;
+  const int first = min((int)threadIdx.x * per, pairs);
+  u64 own = 0;
+  for (int i = first; i < min(first + per, pairs); ++i) own += PairBlocks(p, PairView(p, i), keys, rows).units(p, keys, rows);
+  const u64 inc = wave_scan(own);
+  if ((threadIdx.x & 63) == 63) s.wave[threadIdx.x >> 6] = inc;
+  __syncthreads();
+  u64 at = inc - own;
+  Spans sp;
+  sp.total = 0;
+#pragma unroll
+  for (int v = 0; v < THREADS / 64; ++v) {
+    if (v < (int)(threadIdx.x >> 6)) at += s.wave[v];
+    sp.total += s.wave[v];
+  }
+  if (sp.total == 0) return;
+  sp.n = (int)max(1ull, min((u64)gridDim.x, sp.total));
+  if (w >= sp.n) return;
+  const u64 begin = sp.start(w), end = sp.start(w + 1);
+  if (begin >= at && begin < at + own) {
+    for (int i = first;; ++i) {
+      const u64 n = PairBlocks(p, PairView(p, i), keys, rows).units(p, keys, rows);
+      if (begin < at + n) {
+        s.item = i;
+        break;
+      }
+      at += n;
+    }
+    s.at = begin - at;
+  }
+  __syncthreads();
+  int pair = __builtin_amdgcn_readfirstlane(s.item);
+  u64 off = ((u64)(unsigned)__builtin_amdgcn_readfirstlane((int)(s.at >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)s.at);
+  for (u64 pos = begin; pos < end; ++pair, off = 0) {
+    const PairView view = PairView::uniform(p, pair);
+    const PairBlocks pb(p, view, keys, rows);
+    int block = 0, t = 0;
+    if (pb.blocks == 0) continue;
+    if (off < (u64)pb.whole * pb.tiles) {
+      block = (int)(off / pb.tiles);
+      t = (int)(off - (u64)block * pb.tiles);
+    } else {
+      off -= (u64)pb.whole * pb.tiles;
+      block = pb.whole;
+      for (int n; off >= (u64)(n = pb.tiles - pb.first_tile(p, block, keys, rows)); ++block) off -= n;
+      t = pb.first_tile(p, block, keys, rows) + (int)off;
+    }
+    for (; block < pb.blocks && pos < end; ++block) {
+      const int t_first = block < pb.whole ? 0 : pb.first_tile(p, block, keys, rows);
+      if (t < t_first) t = t_first;
+      const int take = (int)min((u64)(pb.tiles - t), end - pos);
+      WeightSegment seg{pair, block, t, t + take, 2 * w + (pos == begin ? 0 : 1), t == t_first && t + take == pb.tiles};
+      if (t == t_first && threadIdx.x == 0)
+        p.w_joins[(long long)pair * p.w_blocks + block] = int4{w, seg.whole ? w : sp.owner(pos + (pb.tiles - t) - 1), seg.slot, 0};
+      f(seg, view);
+      pos += take;
+      t = 0;
+    }
+  }
 }
-// The tiles of `rows` query rows that this workgroup goes through: those whose last token sees cache row j0, its share of them.
-__device__ __forceinline__ void tile_range(const AttnParams& p, const PairView& w, int j0, int rows, int& begin, int& end) {
-  const int t_first = p.c.causal ? max(0, j0 - (w.end - w.cnt)) : 0;
-  const int first = (int)min((long long)t_first * p.c.G, (long long)w.M) / rows, n = cdiv(w.M, rows) - first;
-  begin = first + (int)((long long)n * blockIdx.z / p.w_splits);
-  end = first + (int)((long long)n * (blockIdx.z + 1) / p.w_splits);
+
+// Sum over the 32 lanes of a half wavefront, on the vector ALU; every lane gets it.
+__device__ __forceinline__ float half_lanes_sum(float v) {
+  v = row_lanes_sum<16>(v);
+  const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r.x) + __uint_as_float(r.y);
+}
+
+// A row's sum of this workgroup's tiles.
+__device__ __forceinline__ void put_weight(const AttnParams& p, const WeightSegment& seg, int keys, int at_block, int j, float v) {
+  if (seg.whole) {
+    const long long at = (long long)seg.pair * rows_cap(p.pg) + j;
+    p.acc_out[at] = (p.acc_in ? p.acc_in[at] : 0.f) + v;
+  } else {
+    p.w_part[(long long)seg.slot * keys + at_block] = v;
+  }
 }
 
 // fp32.  Weights from the finished log-sum-exps: a wavefront owns 32 cache rows, the query rows pass by.
-// grid: (blocks of kRows cache rows, pairs, splits of the query rows)
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_weights_f32_kernel(AttnParams p) {
   __shared__ __attribute__((aligned(16))) float sQ[32 * (D + 4)];
   __shared__ float sL[32];
   __shared__ int sVis[32];
+  __shared__ Scan scan;
   const Chunk& c = p.c;
-  const PairView w(p, blockIdx.y);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, ln = lane & 31, h = lane >> 5;
-  const int j0 = blockIdx.x * kRows + wave * 32;
-  if ((int)blockIdx.x * kRows >= w.end) return;
+  for_weight_segments<kThreads>(p, scan, kRows, 32, [&](const WeightSegment& seg, const PairView& w) {
+  const int j0 = seg.block * kRows + wave * 32;
   const int row = j0 + ln < w.end ? pool_row(p.pg, w.pair, j0 + ln) : -1;
   const unsigned there = (unsigned)__ballot(row >= 0) >> (4 * h);
   float k[D / 2];
@@ -53,9 +144,7 @@ __global__ __launch_bounds__(kThreads) void paged_weights_f32_kernel(AttnParams 
 #pragma unroll
   for (int i = 0; i < 16; ++i) sum[i] = 0.f;
   constexpr int CPR = D / 4;
-  int t0, t1;
-  tile_range(p, w, blockIdx.x * kRows, 32, t0, t1);
-  for (int r0 = t0 * 32; r0 < t1 * 32; r0 += 32) {
+  for (int r0 = seg.t0 * 32; r0 < seg.t1 * 32; r0 += 32) {
     __syncthreads();
     for (int i = threadIdx.x; i < 32 * CPR; i += kThreads) {
       const int r = r0 + i / CPR;
@@ -99,172 +188,176 @@ __global__ __launch_bounds__(kThreads) void paged_weights_f32_kernel(AttnParams 
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
     const int j = j0 + 8 * (i / 4) + 4 * h + i % 4;
-    if (ln == 0 && j < w.end) put_weight(p, w, j, v);
+    if (ln == 0 && j < w.end) put_weight(p, seg, kRows, j - seg.block * kRows, j, v);
   }
+  });
 }
 
-// bf16, many query rows.  A wavefront keeps 64 cache rows as fragments in registers and its 64 sums per lane-half; tiles of 64 query
-// rows pass through LDS, two buffers, one barrier a tile.  Per 64 x 32 weights a wavefront issues 16 matrix instructions (512 cycles)
-// and 32 times scale, 2^x and sum (768 cycles): the vector ALU bounds it, two wavefronts per SIMD overlap the two.
-constexpr int kBfKeys = 64, kBfRows = kWaves * kBfKeys, kBfQ = 64;
+// bf16, many query rows.  A wavefront keeps 64 cache rows as fragments in registers and its sums per lane half; tiles of 64 query
+// rows go from memory straight into a ring of four LDS stages, three on their way while one is worked on, one barrier a tile.  (One
+// tile ahead through registers the loads' latency was the time of a tile: 238 us / W_US for 500 new tokens in four sequences of 8200
+// to 16400 rows.)  The scores of 32 query rows are formed under the weights of the 32 before: per 64 x 32 weights a wavefront
+// issues 16 matrix instructions (512 cycles) and 32 times scale, 2^x and sum (about 600).
+constexpr int kBfKeys = 64, kBfRows = kWaves * kBfKeys, kBfQ = 64, kBfStages = 4;
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void paged_weights_bf16_kernel(AttnParams p) {
-  constexpr int RB = D * 2, QP = RB + 16, CPR = D / 8, KS = D / 16, NL = kBfQ * CPR / kThreads;
-  __shared__ __attribute__((aligned(16))) unsigned char sQ[2][kBfQ * QP];
-  __shared__ long long sAt[2][kBfQ];
-  __shared__ float sRef[4][kBfQ];
-  __shared__ int sVis[4][kBfQ];
+  constexpr int RB = D * 2, CPR = D / 8, KS = D / 16, RPI = 1024 / RB, NL = kBfQ * RB / 1024 / kWaves, LPT = NL + 1;
+  constexpr int kTileBytes = kBfQ * RB;
+  __shared__ __attribute__((aligned(1024))) unsigned char sQ[kBfStages * kTileBytes];
+  __shared__ __attribute__((aligned(256))) float sLse[kBfStages][kWaves][kBfQ];       // a copy per wavefront: its own loads
+  __shared__ Scan scan;
   const Chunk& c = p.c;
-  const PairView w = PairView::uniform(p, blockIdx.y);
-  if ((int)blockIdx.x * kBfRows >= w.end) return;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id(), ln = lane & 31, h = lane >> 5;
-  const int j0 = blockIdx.x * kBfRows + wave * kBfKeys;
   const u16* Kp = static_cast<const u16*>(p.pg.K);
+  const unsigned q_base = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)sQ;
+  const unsigned lse_base = (unsigned)(size_t)(__attribute__((address_space(3))) float*)&sLse[0][wave][0];
   const float c2 = c.scale * kLog2e;
-  bf16x8 kf[2][KS];
-  unsigned there[2];
+  // Steps of kCopyRows rows and of a tile: heads of the group, elements, elements where the head passes the last one.
+  constexpr int kCopyRows = kWaves * RPI;
+  const int copy_dh = kCopyRows % c.G, stat_dh = kBfQ % c.G;
+  const long long copy_step = copy_dh * c.qs[1] + kCopyRows / c.G * c.qs[2], copy_wrap = copy_step - c.G * c.qs[1] + c.qs[2];
+  const long long stat_step = (long long)stat_dh * c.n_new + kBfQ / c.G, stat_wrap = stat_step - (long long)c.G * c.n_new + 1;
+  // the piece of its row that a lane copies: rows change the places of their pieces as in the attention kernels
+  const int in_tile = wave * RPI + lane / CPR, piece = (lane % CPR) ^ (D == 128 ? in_tile & 15 : in_tile >> 1 & 7);
+  typedef __attribute__((address_space(3))) bf16x8* lds_eights;
+  for_weight_segments<kThreads>(p, scan, kBfRows, kBfQ, [&](const WeightSegment& seg, const PairView& w) {
+    const int j0 = seg.block * kBfRows + wave * kBfKeys, t0 = seg.t0, t1 = seg.t1;
+    // The row that this lane copies next and the log-sum-exp it copies next: place, and head of the group, moved on by fixed steps of
+    // tokens and heads.  Rows behind the last one are copied from the pair's first.
+    const u16* q_first = static_cast<const u16*>(p.Q) + w.b * c.qs[0] + w.g * c.G * c.qs[1] + piece * 8;
+    const float* lse_first = p.lse + ((long long)w.b * c.Hq + w.g * c.G) * c.n_new;
+    int copy_row = t0 * kBfQ + wave * RPI + lane / CPR, stat_row = t0 * kBfQ + lane;
+    int copy_h = copy_row % c.G, stat_h = stat_row % c.G;
+    const u16* copy_at = q_first + copy_h * c.qs[1] + copy_row / c.G * c.qs[2];
+    const float* stat_at = lse_first + (long long)stat_h * c.n_new + stat_row / c.G;
+    auto issue = [&](int tile) {
+      const int stage = tile % kBfStages;
 #pragma unroll
-  for (int kb = 0; kb < 2; ++kb) {
-    const int j = j0 + kb * 32 + ln, row = j < w.end ? pool_row(p.pg, w.pair, j) : -1;
-    there[kb] = (unsigned)__ballot(row >= 0);
+      for (int i = 0; i < NL; ++i) {
+        gload_lds16(copy_row < w.M ? copy_at : q_first, q_base + stage * kTileBytes + (i * kWaves + wave) * 1024);
+        copy_row += kCopyRows;
+        copy_h += copy_dh;
+        const bool wrap = copy_h >= c.G;
+        copy_h -= wrap ? c.G : 0;
+        copy_at += wrap ? copy_wrap : copy_step;
+      }
+      gload_lds4(stat_row < w.M ? stat_at : lse_first, lse_base + stage * (kWaves * kBfQ * 4));
+      stat_row += kBfQ;
+      stat_h += stat_dh;
+      const bool wrap = stat_h >= c.G;
+      stat_h -= wrap ? c.G : 0;
+      stat_at += wrap ? stat_wrap : stat_step;
+    };
+    __syncthreads();                                     // the segment before is done with the ring
+    wait_vmcnt<0>();                                     // nothing older is counted below
+    issue(t0);
+    issue(t0 + 1);                                       // tiles behind the last one: nobody reads them
+    issue(t0 + 2);
+    bf16x8 kf[2][KS];
+    unsigned there[2];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      u32x4 raw = {0u, 0u, 0u, 0u};
-      if (row >= 0) raw = *reinterpret_cast<const u32x4*>(Kp + (long long)row * D + ks * 16 + h * 8);
-      kf[kb][ks] = __builtin_bit_cast(bf16x8, raw);
-    }
-  }
-  const bool all_there = (there[0] & there[1]) == 0xffffffffu;
-  float sum[2][16];
+    for (int kb = 0; kb < 2; ++kb) {
+      const int j = j0 + kb * 32 + ln, row = j < w.end ? pool_row(p.pg, w.pair, j) : -1;
+      there[kb] = (unsigned)__ballot(row >= 0);
 #pragma unroll
-  for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum[kb][i] = 0.f;
-
-  int t0, t1;
-  tile_range(p, w, blockIdx.x * kBfRows, kBfQ, t0, t1);
-  // Where the rows of a tile lie and what they see, by the first wavefront: its rows advance by a tile per call of meta_load, and what
-  // it loads is written down a tile later, when it has arrived (a wait for it in between would be one for the query rows, too).
-  int meta_t = (t0 * kBfQ + (int)threadIdx.x) / c.G, meta_h = (t0 * kBfQ + (int)threadIdx.x) - meta_t * c.G;
-  const int step_t = kBfQ / c.G, step_h = kBfQ - step_t * c.G;
-  long long m_at = 0;
-  float m_lse = 0.f;
-  int m_vis = 0;
-  auto meta_load = [&](int tile) {
-    if (threadIdx.x < kBfQ) {
-      const bool real = tile < t1 && meta_t < w.cnt;
-      const int t = real ? meta_t : 0, head = w.g * c.G + (real ? meta_h : 0);
-      m_at = w.b * c.qs[0] + head * c.qs[1] + t * c.qs[2];
-      m_lse = p.lse[((long long)w.b * c.Hq + head) * c.n_new + t];
-      m_vis = real ? w.visible(p, t) : 0;
-      meta_t += step_t;
-      meta_h += step_h;
-      if (meta_h >= c.G) {
-        meta_h -= c.G;
-        ++meta_t;
+      for (int ks = 0; ks < KS; ++ks) {
+        u32x4 raw = {0u, 0u, 0u, 0u};
+        if (row >= 0) raw = *reinterpret_cast<const u32x4*>(Kp + (long long)row * D + ks * 16 + h * 8);
+        kf[kb][ks] = __builtin_bit_cast(bf16x8, raw);
       }
     }
-  };
-  auto meta_write = [&](int tile) {
-    if (threadIdx.x < kBfQ) {
-      sAt[tile & 1][threadIdx.x] = m_at;
-      sRef[tile & 3][threadIdx.x] = m_lse > -INFINITY ? m_lse * kLog2e : 0.f;
-      sVis[tile & 3][threadIdx.x] = m_lse > -INFINITY ? m_vis : 0;
-    }
-  };
-  u32x4 raw[NL];
-  auto load = [&](int tile) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int piece = i * kThreads + threadIdx.x;
-      raw[i] = *reinterpret_cast<const u32x4*>(static_cast<const u16*>(p.Q) + sAt[tile & 1][piece / CPR] + piece % CPR * 8);
-    }
-  };
-  if (t0 < t1) {
-    meta_load(t0);
-    meta_write(t0);
-    meta_load(t0 + 1);
-    meta_write(t0 + 1);
-    __syncthreads();
-    load(t0);
-    meta_load(t0 + 2);
-    __syncthreads();
-  }
-  // Scores of 32 query rows under the weights of the 32 before: each matrix instruction is followed by its share of the vector work.
-  // (One after the other the two wavefronts of a SIMD, which the barrier keeps in step, are in the same phase: 223 us / W_US for 500 new
-  // tokens in four sequences of 8200 to 16400 rows.)
-  float ref_a = 0.f, ref_b = 0.f;
-  f32x16 sa[2], sb[2];
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-  for (int kb = 0; kb < 2; ++kb)
+      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(kf[kb][ks]));          // loaded here, not waited for in the loop
+    // from this tile on every query row sees all of this wavefront's 64 rows: token j0 + 63 - (end - cnt) sees the last one
+    const int clear_t = c.causal ? max(0, j0 + kBfKeys - 1 - (w.end - w.cnt)) : 0;
+    const int clear = (int)min(((long long)clear_t * c.G + kBfQ - 1) / kBfQ, (long long)t1);
+    float sum[2][16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sb[kb][i] = -INFINITY;
-  auto add_weights = [&](const f32x16 (&s)[2], int x, float ref) { sum[x / 16][x % 16] += fast_exp2(fmaf(s[x / 16][x % 16], c2, -ref)); };
-  auto block = [&](int tile, int qb, f32x16 (&s)[2], float& ref, const f32x16 (&old)[2], float old_ref) {
-    const unsigned char* q = &sQ[tile & 1][(qb * 32 + ln) * QP + h * 16];
-    const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    bf16x8 qf[2] = {*reinterpret_cast<const bf16x8*>(q), *reinterpret_cast<const bf16x8*>(q + 32)};
-    constexpr int PER = 16 / KS;                         // weights per matrix instruction: 2 KS of them, 32 weights
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-    for (int x = 0; x < 2 * KS; ++x) {
-      const int kb = x % 2, ks = x / 2;
-      __builtin_amdgcn_sched_barrier(0);
-      s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kb][ks], qf[ks % 2], ks == 0 ? zero16 : s[kb], 0, 0, 0);
-      if (kb == 1 && ks + 2 < KS) qf[ks % 2] = *reinterpret_cast<const bf16x8*>(q + (ks + 2) * 32);
+      for (int i = 0; i < 16; ++i) sum[kb][i] = 0.f;
+    float ref_a = 0.f, ref_b = 0.f;
+    f32x16 sa[2], sb[2];
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        add_weights(old, x * PER + e, old_ref);
-        asm volatile("" : "+v"(sum[(x * PER + e) / 16][(x * PER + e) % 16]));      // here, not behind the branch below
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    ref = sRef[tile & 3][qb * 32 + ln];
-    const int rel = sVis[tile & 3][qb * 32 + ln] - j0;
-    if (!all_there || __any(rel < kBfKeys)) {
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int i = 0; i < 16; ++i) sb[kb][i] = -INFINITY;
+    auto add_weights = [&](const f32x16 (&s)[2], int x, float ref) { sum[x / 16][x % 16] += fast_exp2(fmaf(s[x / 16][x % 16], c2, -ref)); };
+    auto block = [&](int tile, int qb, f32x16 (&s)[2], float& ref, const f32x16 (&old)[2], float old_ref) {
+      const int stage = tile % kBfStages;
+      const unsigned q = q_base + stage * kTileBytes + (qb * 32 + ln) * RB + ((h ^ (D == 128 ? ln & 15 : ln >> 1 & 7)) * 16);
+      const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      auto frag = [&](int ks) { return *(lds_eights)(size_t)(q ^ (ks * 32)); };
+      bf16x8 qf[2] = {frag(0), frag(1)};
+      constexpr int PER = 16 / KS;                       // weights per matrix instruction: 2 KS of them, 32 weights
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = kb * 32 + 8 * (i / 4) + 4 * h + i % 4;
-          if (key >= rel || !((there[kb] >> (key & 31)) & 1u)) s[kb][i] = -INFINITY;
+      for (int x = 0; x < 2 * KS; ++x) {
+        const int kb = x % 2, ks = x / 2;
+        __builtin_amdgcn_sched_barrier(0);
+        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kb][ks], qf[ks % 2], ks == 0 ? zero16 : s[kb], 0, 0, 0);
+        if (kb == 1 && ks + 2 < KS) qf[ks % 2] = frag(ks + 2);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          add_weights(old, x * PER + e, old_ref);
+          asm volatile("" : "+v"(sum[(x * PER + e) / 16][(x * PER + e) % 16]));      // here, not behind the branch below
         }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const float lse = sLse[stage][wave][qb * 32 + ln];
+      ref = lse * kLog2e;
+      if ((tile + 1) * kBfQ > w.M || lse == -INFINITY) {          // behind the last row, or a row that sees nothing: 2^(x - inf) = 0
+        const int r = tile * kBfQ + qb * 32 + ln;
+        if (r >= w.M || lse == -INFINITY) ref = INFINITY;
+      }
+      if (tile < clear) {
+        const int rel = w.visible(p, (tile * kBfQ + qb * 32 + ln) / c.G) - j0 - 4 * h;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (kb * 32 + 8 * (i / 4) + i % 4 >= rel) s[kb][i] = -INFINITY;
+      }
+    };
+    for (int tile = t0; tile < t1; ++tile) {
+      wait_vmcnt<2 * LPT>();                             // this wavefront's share of the tile has landed
+      __syncthreads();                                   // and everyone's; the tile before is done with, its stage is free
+      issue(tile + 3);
+      block(tile, 0, sa, ref_a, sb, ref_b);
+      block(tile, 1, sb, ref_b, sa, ref_a);
     }
-  };
-  for (int tile = t0; tile < t1; ++tile) {
+    wait_vmcnt<0>();                                     // no copy is on its way into a ring that is not this segment's any more
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int piece = i * kThreads + threadIdx.x;
-      *reinterpret_cast<u32x4*>(&sQ[tile & 1][piece / CPR * QP + piece % CPR * 16]) = raw[i];
-    }
-    meta_write(tile + 2);
-    if (tile + 1 < t1) load(tile + 1);
-    meta_load(tile + 3);
-    __syncthreads();
-    block(tile, 0, sa, ref_a, sb, ref_b);
-    block(tile, 1, sb, ref_b, sa, ref_a);
-  }
+    for (int x = 0; x < 32; ++x) add_weights(sb, x, ref_b);
+    // lane ln of a half takes the sum of its row: block ln / 16, register ln % 16
+    float own = 0.f;
 #pragma unroll
-  for (int x = 0; x < 32; ++x) add_weights(sb, x, ref_b);
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-  for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float v = sum[kb][i];
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-      const int j = j0 + kb * 32 + 8 * (i / 4) + 4 * h + i % 4;
-      if (ln == 0 && j < w.end) put_weight(p, w, j, v);
-    }
+      for (int i = 0; i < 16; ++i) {
+        const float v = half_lanes_sum(sum[kb][i]);
+        own = ln == kb * 16 + i ? v : own;
+      }
+    const int in_block = wave * kBfKeys + ln / 16 * 32 + 8 * (ln % 16 / 4) + 4 * h + ln % 4, j = seg.block * kBfRows + in_block;
+    // a row that is not there entered as zeros: nobody attends it
+    if (j < w.end) put_weight(p, seg, kBfRows, in_block, j, (ln < 16 ? there[0] : there[1]) >> (in_block & 31) & 1u ? own : 0.f);
+  });
 }
 
-// The planes of split query rows.  grid: (blocks of cache rows, pairs)
-__global__ __launch_bounds__(kThreads) void paged_weights_sum_kernel(AttnParams p) {
+// Blocks whose tiles were split, and pairs without new tokens.  grid: (blocks of KEYS rows, pairs)
+template <int KEYS>
+__global__ __launch_bounds__(KEYS) void paged_weights_join_kernel(AttnParams p) {
   const PairView w(p, blockIdx.y);
-  const int j = blockIdx.x * kThreads + threadIdx.x;
+  const int j = blockIdx.x * KEYS + threadIdx.x;
   if (j >= w.end) return;
-  const long long at = (long long)w.pair * rows_cap(p.pg) + j, plane = (long long)p.c.B * p.c.Hkv * rows_cap(p.pg);
   float v = 0.f;
-  for (int s = 0; s < p.w_splits; ++s) v += p.w_part[s * plane + at];
+  if (w.M) {
+    const int4 join = p.w_joins[(long long)blockIdx.y * p.w_blocks + blockIdx.x];
+    if (join.x == join.y) return;                        // one workgroup had all of it and wrote the rows
+    for (int i = join.x; i <= join.y; ++i) v += p.w_part[(long long)(i == join.x ? join.z : 2 * i) * KEYS + threadIdx.x];
+  }
+  const long long at = (long long)blockIdx.y * rows_cap(p.pg) + j;
   p.acc_out[at] = (p.acc_in ? p.acc_in[at] : 0.f) + v;
 }
 
@@ -305,31 +398,33 @@ __global__ __launch_bounds__(kThreads) void paged_weights_logits_kernel(AttnPara
 
 }  // namespace
 
-// Workgroups enough for the chip: where the cache rows give few, the query rows are split, a tile or more each.
-int weight_splits(const Chunk& c, int dtype, int cap) {
-  const long long blocks = (long long)c.B * c.Hkv * cdiv(cap, dtype == OMNI_BF16 ? kBfRows : kRows);
-  const int tiles = cdiv(c.G * c.n_new, dtype == OMNI_BF16 ? kBfQ : 32);
-  return (int)max(1ll, min(min((1535 + blocks) / blocks, 16ll), (long long)tiles));
+// What the pass needs: workgroups, blocks of a pair (rows_cap / the rows of a block), floats of the slots.
+WeightPlan weight_plan(int dtype, int cap) {
+  return dtype == OMNI_BF16 ? WeightPlan{512, cdiv(cap, kBfRows), (size_t)2 * 512 * kBfRows}
+                            : WeightPlan{768, cdiv(cap, kRows), (size_t)2 * 768 * kRows};
 }
 
 int launch_weights(const AttnParams& p, int dtype, hipStream_t st) {
   const int pairs = p.c.B * p.c.Hkv, cap = rows_cap(p.pg);
   if (p.logits) {
     paged_weights_logits_kernel<<<dim3(cdiv(cap, 32 * kLogitBlocks), pairs), kThreads, 0, st>>>(p);
-  } else if (dtype == OMNI_BF16) {
-    const dim3 grid(cdiv(cap, kBfRows), pairs, p.w_splits);
-    if (p.c.D == 128) paged_weights_bf16_kernel<128><<<grid, kThreads, 0, st>>>(p);
-    else paged_weights_bf16_kernel<64><<<grid, kThreads, 0, st>>>(p);
+    OMNI_LAUNCH_CHECK();
+    return OMNI_OK;
+  }
+  const WeightPlan pl = weight_plan(dtype, cap);
+  const dim3 blocks(pl.blocks, pairs);
+  if (dtype == OMNI_BF16) {
+    if (p.c.D == 128) paged_weights_bf16_kernel<128><<<pl.n_wgs, kThreads, 0, st>>>(p);
+    else paged_weights_bf16_kernel<64><<<pl.n_wgs, kThreads, 0, st>>>(p);
+    OMNI_LAUNCH_CHECK();
+    paged_weights_join_kernel<kBfRows><<<blocks, kBfRows, 0, st>>>(p);
   } else {
-    const dim3 grid(cdiv(cap, kRows), pairs, p.w_splits);
-    if (p.c.D == 128) paged_weights_f32_kernel<128><<<grid, kThreads, 0, st>>>(p);
-    else paged_weights_f32_kernel<64><<<grid, kThreads, 0, st>>>(p);
+    if (p.c.D == 128) paged_weights_f32_kernel<128><<<pl.n_wgs, kThreads, 0, st>>>(p);
+    else paged_weights_f32_kernel<64><<<pl.n_wgs, kThreads, 0, st>>>(p);
+    OMNI_LAUNCH_CHECK();
+    paged_weights_join_kernel<kRows><<<blocks, kRows, 0, st>>>(p);
   }
   OMNI_LAUNCH_CHECK();
-  if (p.w_splits > 1) {
-    paged_weights_sum_kernel<<<dim3(cdiv(cap, kThreads), pairs), kThreads, 0, st>>>(p);
-    OMNI_LAUNCH_CHECK();
-  }
   return OMNI_OK;
 }
 
