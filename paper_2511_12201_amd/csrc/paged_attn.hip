@@ -39,7 +39,8 @@ __device__ __forceinline__ int swz_v(int row) { return D == 128 ? (row & 3) << 2
 template <int D, bool LOGITS>
 __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnParams p) {
   constexpr int RB = D * 2, CPR = D / 8, RPI = 1024 / RB, NB = D / 32, KS = D / 16;
-  constexpr int kKBytes = 32 * RB, kStageBytes = 2 * kKBytes, LPH = kKBytes / 1024, LPT = 2 * LPH;
+  constexpr int kKBytes = 32 * RB, kStageBytes = 2 * kKBytes, LPH = kKBytes / 1024;
+  constexpr int kStores = LOGITS ? 4 : 0;                // store instructions of a trip
   constexpr int QP = RB + 16;                            // bytes between the queries
   constexpr int OP = 36;                                 // floats between the rows of the merge buffer (32 of the D elements at a time)
   __shared__ __attribute__((aligned(1024))) unsigned char ring[kStreamWaves * 2 * kStageBytes];
@@ -70,41 +71,41 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
     const PairView w = PairView::uniform(p, seg.pair);
     const int keys = w.visible(p, (w.M - 1) / c.G);
     const int first = seg.u0 * kStreamWaves + wave, last = min(seg.u1 * kStreamWaves, cdiv(keys, 32));
-    const int* table = p.pg.table + (long long)seg.pair * p.pg.pages_cap;
+    // read only while the kernel runs: entries come through the scalar cache, so that no wait for them is one for the copies
+    const auto* table = (const __attribute__((address_space(4))) int*)(p.pg.table + (long long)seg.pair * p.pg.pages_cap);
     const int page_mask = (1 << p.pg.shift) - 1;
-    // pool rows of a block's two halves of 16 rows (each inside one page), -1: not there
-    auto half_row = [&](int block, int half) {
+    // table entries of a block's two halves of 16 rows (each inside one page), and the pool row of a half, -1: not there
+    auto entry = [&](int block, int half) {
       const int j = block * 32 + half * 16;
-      if (block >= last || j >= w.end) return -1;
-      const int page = __builtin_amdgcn_readfirstlane(table[j >> p.pg.shift]);
-      return (unsigned)page < (unsigned)p.pg.n_pages ? (page << p.pg.shift) + (j & page_mask) : -1;
+      return block < last && j < w.end ? (int)table[j >> p.pg.shift] : -1;
     };
-    auto issue = [&](int block, int stage, int row_a, int row_b) {
-      const unsigned dst = own_ring + stage * kStageBytes;
+    auto half_row = [&](int block, int half, int page) {
+      return (unsigned)page < (unsigned)p.pg.n_pages ? (page << p.pg.shift) + ((block * 32 + half * 16) & page_mask) : -1;
+    };
+    // K or V of a block into a stage
+    auto issue = [&](auto is_k, int block, int stage, int row_a, int row_b) {
+      constexpr bool kIsK = decltype(is_k)::value;
+      const unsigned char* pool = kIsK ? Kpool : Vpool;
+      const int at = stage * kStageBytes + (kIsK ? 0 : kKBytes);
       if (row_a >= 0 && row_b >= 0 && block * 32 + 32 <= w.end) {
 #pragma unroll
         for (int i = 0; i < LPH; ++i) {
           const long long row = (long long)(i * RPI < 16 ? row_a : row_b) + i * RPI % 16;
-          gload_lds16(Kpool + row * RB, src_k[i % NP], dst + i * 1024);
-          gload_lds16(Vpool + row * RB, src_v, dst + kKBytes + i * 1024);
+          gload_lds16(pool + row * RB, kIsK ? src_k[i % NP] : src_v, own_ring + at + i * 1024);
         }
-      } else {                                           // zeros for what is not there; these loads end here
+      } else {                                           // zeros for what is not there; these loads end here, and so do all before
 #pragma unroll
         for (int i = 0; i < LPH; ++i) {
           const int r = i * RPI + in_row, from = r < 16 ? row_a : row_b;
-          u32x4 k = {0u, 0u, 0u, 0u}, v = k;
-          if (from >= 0 && block * 32 + r < w.end) {
-            const long long at = ((long long)from + r % 16) * RB + slot * 16;
-            k = *reinterpret_cast<const u32x4*>(Kpool + at);
-            v = *reinterpret_cast<const u32x4*>(Vpool + at);
-          }
-          unsigned char* to = own_bytes + stage * kStageBytes + r * RB;
-          *reinterpret_cast<u32x4*>(to + (slot ^ swz_k<D>(r)) * 16) = k;
-          *reinterpret_cast<u32x4*>(to + kKBytes + (slot ^ swz_v<D>(r)) * 16) = v;
+          u32x4 x = {0u, 0u, 0u, 0u};
+          if (from >= 0 && block * 32 + r < w.end) x = *reinterpret_cast<const u32x4*>(pool + ((long long)from + r % 16) * RB + slot * 16);
+          *reinterpret_cast<u32x4*>(own_bytes + at + r * RB + (slot ^ (kIsK ? swz_k<D>(r) : swz_v<D>(r))) * 16) = x;
         }
       }
     };
-    int row_a = half_row(first, 0), row_b = half_row(first, 1);
+    constexpr std::true_type kKeys{};
+    constexpr std::false_type kValues{};
+    int row_a = half_row(first, 0, entry(first, 0)), row_b = half_row(first, 1, entry(first, 1));
     __syncthreads();                                     // the last segment's queries and merge buffer are done with
     for (int i = threadIdx.x; i < 32 * CPR; i += kStreamThreads) {
       const int r = i / CPR;
@@ -116,8 +117,19 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
       *reinterpret_cast<u32x4*>(sQ + r * QP + i % CPR * 16) = raw;
     }
     wait_vmcnt<0>();                                     // nothing older is counted below
-    if (first < last) issue(first, 0, row_a, row_b);
-    int next_a = half_row(first + kStreamWaves, 0), next_b = half_row(first + kStreamWaves, 1);
+    // K(0) V(0) K(1) V(1) .. are issued in this order, a block's K two trips ahead as soon as its stage's keys are read, its V as
+    // soon as the values are: three halves of a stage or more are always on their way
+    const int second = first + kStreamWaves;
+    int row_a1 = half_row(second, 0, entry(second, 0)), row_b1 = half_row(second, 1, entry(second, 1));
+    if (first < last) {
+      issue(kKeys, first, 0, row_a, row_b);
+      issue(kValues, first, 0, row_a, row_b);
+    }
+    if (second < last) {
+      issue(kKeys, second, 1, row_a1, row_b1);
+      issue(kValues, second, 1, row_a1, row_b1);
+    }
+    int page_a2 = entry(second + kStreamWaves, 0), page_b2 = entry(second + kStreamWaves, 1);
     const int vis = n < w.M ? w.visible(p, n / c.G) : 0;
     f32x16 o[NB];
 #pragma unroll
@@ -132,23 +144,25 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
     int stage = 0;
     for (int block = first; block < last; block += kStreamWaves) {
       const unsigned there = ((row_a >= 0 ? 0xffffu : 0u) | (row_b >= 0 ? 0xffff0000u : 0u)) >> (4 * h);
-      row_a = next_a;
-      row_b = next_b;
-      if (block + kStreamWaves < last) {
-        issue(block + kStreamWaves, stage ^ 1, row_a, row_b);
-        next_a = half_row(block + 2 * kStreamWaves, 0);
-        next_b = half_row(block + 2 * kStreamWaves, 1);
-        wait_vmcnt<LPT>();
-      } else {
-        wait_vmcnt<0>();
-      }
+      const bool next = block + kStreamWaves < last, next2 = block + 2 * kStreamWaves < last;
+      // K of this block has landed: newer are its V, the next block and, from the second trip on, the stores of at least one trip
+      if (!next) wait_vmcnt<LPH>();
+      else if (block == first) wait_vmcnt<3 * LPH>();
+      else wait_vmcnt<3 * LPH + kStores>();
       const unsigned base = own_ring + stage * kStageBytes;
       f32x16 s;
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = 0.f;
+      bf16x8 kf[KS];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(lds_eights)(size_t)((base + frag_k) ^ (ks * 32)), qf[ks], s, 0, 0, 0);
+      for (int ks = 0; ks < KS; ++ks) kf[ks] = *(lds_eights)(size_t)((base + frag_k) ^ (ks * 32));
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the keys are read: their stage is free
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], s, 0, 0, 0);
+      const int row_a2 = half_row(block + 2 * kStreamWaves, 0, page_a2), row_b2 = half_row(block + 2 * kStreamWaves, 1, page_b2);
+      page_a2 = entry(block + 3 * kStreamWaves, 0);
+      page_b2 = entry(block + 3 * kStreamWaves, 1);
+      if (next2) issue(kKeys, block + 2 * kStreamWaves, stage, row_a2, row_b2);
       const int rel = min(vis, w.end) - block * 32 - 4 * h;   // rows of this block from here on are not seen
       float mx = m;
 #pragma unroll
@@ -185,17 +199,29 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
       union { bf16x8 v[2]; unsigned u[8]; } pf;
 #pragma unroll
       for (int i = 0; i < 16; i += 2) pf.u[i / 2] = pack_bf16x2(s[i], s[i + 1]);
+      // V of this block has landed: newer are the next block, the K after it and this trip's stores
+      if (next2) wait_vmcnt<3 * LPH + kStores>();
+      else if (next) wait_vmcnt<2 * LPH>();
+      else wait_vmcnt<0>();
+      union { s16x4 q[2]; bf16x8 v; } vf[2][NB];
 #pragma unroll
       for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
         for (int db = 0; db < NB; ++db) {
-          union { s16x4 q[2]; bf16x8 v; } vf;
           const unsigned at = ((base + frag_v) ^ (db * 64)) + s2 * 16 * RB;
-          vf.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quads)(size_t)at);
-          vf.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quads)(size_t)(at + 8 * RB));
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.v, pf.v[s2], o[db], 0, 0, 0);
+          vf[s2][db].q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quads)(size_t)at);
+          vf[s2][db].q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quads)(size_t)(at + 8 * RB));
         }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // this stage is read: the next trip's copies may overwrite it
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // and the values
+      if (next2) issue(kValues, block + 2 * kStreamWaves, stage, row_a2, row_b2);
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+        for (int db = 0; db < NB; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s2][db].v, pf.v[s2], o[db], 0, 0, 0);
+      row_a = row_a1;
+      row_b = row_b1;
+      row_a1 = row_a2;
+      row_b1 = row_b2;
       stage ^= 1;
     }
     // join the wavefronts in their order, 32 elements of the rows at a time

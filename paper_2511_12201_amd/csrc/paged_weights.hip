@@ -363,7 +363,7 @@ __global__ __launch_bounds__(KEYS) void paged_weights_join_kernel(AttnParams p) 
 
 // The same from scores that the pass over the cache has kept (few query rows): a wavefront takes 32 cache rows at a time, two
 // query rows per load.  grid: (blocks of cache rows, pairs)
-constexpr int kLogitBlocks = 16;                         // 32-row blocks of a workgroup
+constexpr int kLogitBlocks = 4;                          // 32-row blocks of a workgroup
 __global__ __launch_bounds__(kThreads) void paged_weights_logits_kernel(AttnParams p) {
   __shared__ float sL[32];
   const PairView w(p, blockIdx.y);
