@@ -1138,6 +1138,7 @@ int omni_paged_attn(const omni_chunk_desc* desc, const void* Q, const omni_page_
   CHECK(validate_chunk(desc));
   REQUIRE_PTR(Q); REQUIRE_PTR(row_end); REQUIRE_PTR(new_cnt); REQUIRE_PTR(O); REQUIRE_PTR(lse);
   REQUIRE_ALIGNED(Q); REQUIRE_ALIGNED(O);
+  REQUIRE_ALIGNED(acc_in); REQUIRE_ALIGNED(acc_out);
   if (acc_in && !acc_out) OMNI_FAIL(OMNI_ERR_INVALID, "acc_in without acc_out");
   if (O == Q) OMNI_FAIL(OMNI_ERR_INVALID, "O must not be Q");
   Pages pg;

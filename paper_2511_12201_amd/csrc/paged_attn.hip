@@ -40,11 +40,14 @@ template <int D, bool LOGITS>
 __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnParams p) {
   constexpr int RB = D * 2, CPR = D / 8, RPI = 1024 / RB, NB = D / 32, KS = D / 16;
   constexpr int kKBytes = 32 * RB, kStageBytes = 2 * kKBytes, LPH = kKBytes / 1024;
-  constexpr int kStores = LOGITS ? 4 : 0;                // store instructions of a trip
+  constexpr int kStores = LOGITS ? 1 : 0;                // store instructions of a trip, at least
+  constexpr int kScoreBytes = 16 * 128;                  // scores of 16 query rows on their way out, of a wavefront
   constexpr int QP = RB + 16;                            // bytes between the queries
   constexpr int OP = 36;                                 // floats between the rows of the merge buffer (32 of the D elements at a time)
   __shared__ __attribute__((aligned(1024))) unsigned char ring[kStreamWaves * 2 * kStageBytes];
-  __shared__ __attribute__((aligned(16))) unsigned char sQ[32 * QP];
+  // the queries, which go into registers; with LOGITS then the wavefronts' scores on their way out
+  constexpr int kSharedBytes = LOGITS && kStreamWaves * kScoreBytes > 32 * QP ? kStreamWaves * kScoreBytes : 32 * QP;
+  __shared__ __attribute__((aligned(16))) unsigned char sQ[kSharedBytes];
   __shared__ float sM[kStreamWaves][32], sL[kStreamWaves][32];
   __shared__ Scan scan;
   static_assert(kStreamWaves * 32 * OP * 4 <= (int)sizeof(ring), "the merge buffer takes the ring's place");
@@ -141,6 +144,7 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
     bf16x8 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(qlane + ks * 32);
+    if constexpr (LOGITS) __syncthreads();               // everyone has them
     int stage = 0;
     for (int block = first; block < last; block += kStreamWaves) {
       const unsigned there = ((row_a >= 0 ? 0xffffu : 0u) | (row_b >= 0 ? 0xffff0000u : 0u)) >> (4 * h);
@@ -172,11 +176,25 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
         mx = fmaxf(mx, s[i]);
       }
       if constexpr (LOGITS) {
-        if (n < w.M) {
-          const int mfull = c.G * c.n_new;
-          float* dst = p.logits + (((long long)w.pair * cdiv(rows_cap(p.pg), 32) + block) * mfull + n) * 32 + 4 * h;
+        // through LDS, so that a store writes whole lines: rows of 32 scores, 8 of them per instruction (16 bytes a lane straight from
+        // the accumulators, a quarter of a line per instruction: no faster with 117 MB of them beside 2.1 GB of rows, but the pass that adds them up reads them at 4.6 TB/s)
+        unsigned char* out = sQ + wave * kScoreBytes;
+        float* dst = p.logits + ((long long)w.pair * cdiv(rows_cap(p.pg), 32) + block) * (c.G * c.n_new) * 32;
 #pragma unroll
-          for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(dst + 2 * i) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
+        for (int half = 0; half < 2; ++half) {
+          if (half * 16 >= w.M) break;
+          if (n / 16 == half) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+              *reinterpret_cast<f32x4*>(out + n % 16 * 128 + ((i / 2 + h) ^ (n & 7)) * 16) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int r = k * 8 + lane / 8;
+            if (half * 16 + k * 8 >= w.M) break;
+            const f32x4 x = *reinterpret_cast<const f32x4*>(out + r * 128 + ((lane ^ r) & 7) * 16);
+            if (half * 16 + r < w.M) *reinterpret_cast<f32x4*>(dst + (half * 16 + r) * 32 + lane % 8 * 4) = x;
+          }
         }
       }
       mx = pair_max(mx);

@@ -361,16 +361,35 @@ __global__ __launch_bounds__(KEYS) void paged_weights_join_kernel(AttnParams p) 
   p.acc_out[at] = (p.acc_in ? p.acc_in[at] : 0.f) + v;
 }
 
-// The same from scores that the pass over the cache has kept (few query rows): a wavefront takes 32 cache rows at a time, two
-// query rows per load.  grid: (blocks of cache rows, pairs)
-constexpr int kLogitBlocks = 4;                          // 32-row blocks of a workgroup
+// The same from scores that the pass over the cache has kept (few query rows).  A block of 32 cache rows is M rows of 32 scores: a lane
+// takes 4 neighbours, so that one load is 8 query rows, and a wavefront works on four blocks at once; memory bounds it.
+// grid: (blocks of cache rows, pairs)
+constexpr int kLogitBlocks = 4 * kWaves;                 // 32-row blocks of a workgroup
 __global__ __launch_bounds__(kThreads) void paged_weights_logits_kernel(AttnParams p) {
   __shared__ float sL[32];
-  const PairView w(p, blockIdx.y);
-  const int first = blockIdx.x * kLogitBlocks;
-  if (first * 32 >= w.end) return;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, ln = lane & 31, h = lane >> 5;
-  const int mfull = p.c.G * p.c.n_new, cap = rows_cap(p.pg);
+  const PairView w = PairView::uniform(p, blockIdx.y);
+  if ((int)blockIdx.x * kLogitBlocks * 32 >= w.end) return;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id(), r0 = lane / 8, quad = lane % 8;
+  const int mfull = p.c.G * p.c.n_new, cap = rows_cap(p.pg), blocks = cdiv(w.end, 32);
+  const int first = blockIdx.x * kLogitBlocks + wave * 4;
+  // the first eight rows' scores and the weights so far are on their way while the log-sum-exps arrive
+  f32x4 x[4], sum[4];
+  auto load = [&](int r) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      x[k] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      if (first + k < blocks && r < w.M)
+        x[k] = *reinterpret_cast<const f32x4*>(p.logits + (((long long)w.pair * cdiv(cap, 32) + first + k) * mfull + r) * 32 + quad * 4);
+    }
+  };
+  load(r0);
+  // lanes 0..7 hold the four rows of the first block, 8..15 of the second, ..: block lane / 8 % 4
+  const int j = (first + r0 % 4) * 32 + quad * 4;
+  const long long at = (long long)w.pair * cap + j;
+  f32x4 own = {0.f, 0.f, 0.f, 0.f};
+  if (lane < 32 && p.acc_in && j + 3 < w.end) own = *reinterpret_cast<const f32x4*>(p.acc_in + at);
+  else if (lane < 32 && p.acc_in)
+    for (int e = 0; e < 4; ++e) own[e] = j + e < w.end ? p.acc_in[at + e] : 0.f;
   if (threadIdx.x < 32) {
     long long at_lse;
     float ref = 0.f;                                     // a query row that sees nothing: its scores are -inf, its weights 0
@@ -382,17 +401,34 @@ __global__ __launch_bounds__(kThreads) void paged_weights_logits_kernel(AttnPara
     sL[threadIdx.x] = ref;
   }
   __syncthreads();
-  for (int block = first + wave; block < min(first + kLogitBlocks, cdiv(w.end, 32)); block += kWaves) {
-    const float* src = p.logits + ((long long)w.pair * cdiv(cap, 32) + block) * mfull * 32 + lane;
-    const int j = block * 32 + ln;
-    const long long at = (long long)w.pair * cap + j;
-    const float before = h == 0 && j < w.end && p.acc_in ? p.acc_in[at] : 0.f;
-    float sum = 0.f;
-#pragma unroll 4
-    for (int r = 0; r < w.M; r += 2)
-      if (r + h < w.M) sum += fast_exp2(src[r * 32] - sL[r + h]);
-    sum = pair_sum(sum);
-    if (h == 0 && j < w.end) p.acc_out[at] = before + sum;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sum[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int r = r0; r < r0 + 32; r += 8) {
+    if (r - r0 >= w.M) break;
+    if (r != r0) load(r);
+    const float ref = sL[r & 31];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[k][e] += fast_exp2(x[k][e] - ref);
+  }
+  f32x4 mine = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {                        // over the eight rows: lanes 8, 16 and 32 apart
+      float v = sum[k][e];
+      v += __uint_as_float(dpp_or_zero<0x128, 0xf>(__float_as_uint(v)));
+      const u32x2 s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+      v = pair_sum(__uint_as_float(s.x) + __uint_as_float(s.y));
+      mine[e] = r0 % 4 == k ? v : mine[e];
+    }
+  if (lane < 32) {
+    own += mine;
+    if (j + 3 < w.end) *reinterpret_cast<f32x4*>(p.acc_out + at) = own;
+    else
+      for (int e = 0; e < 4; ++e)
+        if (j + e < w.end) p.acc_out[at + e] = own[e];
   }
 }
 

@@ -100,6 +100,7 @@ def test_attention_refuses(lib):
     assert _attn(lib, Q=FAKE + 8) == -1 and _attn(lib, O=FAKE + 8) == -1
     assert _attn(lib, O=FAKE) == -1 and "O must not be Q" in ob.last_error()
     assert _attn(lib, acc_in=FAKE) == -1 and "acc_out" in ob.last_error()
+    assert _attn(lib, acc_out=FAKE + 4) == -1 and "aligned" in ob.last_error()
     assert _attn(lib, ws=FAKE + 16) == -3 and _attn(lib, n=0) == -3
     need = ob.workspace_bytes(ob.CALL_PAGED_ATTN, _chunk(), 128)
     assert _attn(lib, acc_out=FAKE, n=need - 1) == -3
