@@ -957,14 +957,19 @@ def _scratch(ws: Workspace | None, call_id: int, desc, param: int, dev):
 
 def _pool_of(pool: PagePool, dtype, head_dim: int, dev):
     """(batch, n_kv_heads, rows_cap) of a pool whose tensors fit the call."""
-    K, V, table = pool._keep
-    if K.dtype is not dtype or V.dtype is not dtype or K.shape[-1] != head_dim:
+    facts = getattr(pool, "_facts", None)
+    if facts is None:                             # of the tensors the pool was made of: they do not change
+        K, V, table = pool._keep
+        if table.dim() != 3:
+            raise ValueError("page_table must be [batch, n_kv_heads, pages_cap]")
+        if V.dtype != K.dtype or V.device != K.device or table.device != K.device:
+            raise ValueError("pool tensors and page table must be of one dtype and on one device")
+        facts = pool._facts = K.dtype, K.shape[-1], K.device, (table.shape[0], table.shape[1], pool.pages_cap * pool.page_rows)
+    if facts[0] is not dtype or facts[1] != head_dim:
         raise ValueError("pool dtype / head_dim differ from the call's")
-    if K.device != dev or V.device != dev or table.device != dev:
+    if facts[2] != dev:
         raise ValueError(f"pool and page table must be on {dev}")
-    if table.dim() != 3:
-        raise ValueError("page_table must be [batch, n_kv_heads, pages_cap]")
-    return table.shape[0], table.shape[1], pool.pages_cap * pool.page_rows
+    return facts[3]
 
 
 def _pairs_desc(pool: PagePool) -> ChunkDesc:

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
   typedef __attribute__((address_space(3))) bf16x8* lds_eights;
   const unsigned char* qlane = sQ + n * QP + h * 16;
 
-  for_segments<kStreamThreads>(p, scan, blockIdx.x, [&](const Segment& seg) {
+  for_segments<kStreamThreads>(p, scan, [&](const Segment& seg) {
     const PairView w = PairView::uniform(p, seg.pair);
     const int keys = w.visible(p, (w.M - 1) / c.G);
     const int first = seg.u0 * kStreamWaves + wave, last = min(seg.u1 * kStreamWaves, cdiv(keys, 32));
@@ -353,7 +353,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
   typedef __attribute__((address_space(3))) bf16x8* lds_eights;
   const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
-  for_segments<kTileThreads>(p, scan, blockIdx.x, [&](const Segment& seg) {
+  for_segments<kTileThreads>(p, scan, [&](const Segment& seg) {
     const PairView w = PairView::uniform(p, seg.pair);
     const bool active = seg.r0 + wave * 32 < w.M;        // wave-uniform: the others only copy
     const int rc = min(seg.r0 + wave * 32 + ln, w.M - 1);

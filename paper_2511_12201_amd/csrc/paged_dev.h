@@ -107,13 +107,20 @@ struct Segment {
 };
 
 // Walks a workgroup's span: f(segment) for its part of every item in it.  All threads call it.
+// Neighbouring spans go to one XCD (workgroup b runs on XCD b % 8): they share a pair, and often the place in it.
+__device__ __forceinline__ int span_of(int b, int n) {
+  const int each = n / 8;
+  return b < each * 8 ? b % 8 * each + b / 8 : b;
+}
+
 template <int THREADS, typename F>
-__device__ __forceinline__ void for_segments(const AttnParams& p, Scan& s, int w, F f) {
+__device__ __forceinline__ void for_segments(const AttnParams& p, Scan& s, F f) {
   int first, per;
   u64 own;
   Spans sp;
   u64 at = scan_items<THREADS>(p, s, first, per, own, sp);
-  if (sp.total == 0 || w >= sp.n) return;
+  if (sp.total == 0 || (int)blockIdx.x >= sp.n) return;
+  const int w = span_of(blockIdx.x, sp.n);
   const u64 begin = sp.start(w), end = sp.start(w + 1);
   if (begin >= at && begin < at + own) {
     int i = first;

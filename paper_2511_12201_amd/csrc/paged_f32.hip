@@ -29,7 +29,7 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 1 : 2) void paged_attn_f32_kernel
   const int loader = SPLIT ? lane : (int)threadIdx.x;
   const float c2 = c.scale * kLog2e;
 
-  for_segments<kThreads>(p, scan, blockIdx.x, [&](const Segment& seg) {
+  for_segments<kThreads>(p, scan, [&](const Segment& seg) {
     const PairView w = PairView::uniform(p, seg.pair);
     const int r = seg.r0 + (SPLIT ? 0 : wave * 32) + ln;
     const bool real = r < w.M;

@@ -36,7 +36,7 @@ struct WeightSegment {
 
 template <int THREADS, typename F>
 __device__ __forceinline__ void for_weight_segments(const AttnParams& p, Scan& s, int keys, int rows, F f) {
-  const int pairs = p.c.B * p.c.Hkv, per = cdiv(pairs, THREADS), w = blockIdx.x;
+  const int pairs = p.c.B * p.c.Hkv, per = cdiv(pairs, THREADS);
   const int first = min((int)threadIdx.x * per, pairs);
   u64 own = 0;
   for (int i = first; i < min(first + per, pairs); ++i) own += PairBlocks(p, PairView(p, i), keys, rows).units(p, keys, rows);
@@ -53,7 +53,8 @@ __device__ __forceinline__ void for_weight_segments(const AttnParams& p, Scan& s
   }
   if (sp.total == 0) return;
   sp.n = (int)max(1ull, min((u64)gridDim.x, sp.total));
-  if (w >= sp.n) return;
+  if ((int)blockIdx.x >= sp.n) return;
+  const int w = span_of(blockIdx.x, sp.n);
   const u64 begin = sp.start(w), end = sp.start(w + 1);
   if (begin >= at && begin < at + own) {
     for (int i = first;; ++i) {
