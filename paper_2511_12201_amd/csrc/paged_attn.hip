@@ -366,9 +366,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + ks * 16);
     }
-    // the loads end here: a wait for them inside the loop would wait for the copies in flight, too
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
 
     f32x16 o[NB];
 #pragma unroll
@@ -394,6 +391,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
         if (!there) sMissing = 1;
       }
       __syncthreads();
+      // the loads of the queries end here: a wait for them inside the loop would wait for the copies in flight, too
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
       const bool missing = __builtin_amdgcn_readfirstlane(sMissing) != 0;
       const int n_plain = missing ? 0 : min(nt, w.end / kTileKeys - c0);              // whole tiles come first
       const int n_full = missing ? 0 : min(seen_by_all / kTileKeys - c0, nt);         // tiles in which nothing is masked
@@ -634,78 +634,124 @@ int launch_tiles(const AttnParams& p, hipStream_t st) {
 
 // ------------------------------------------------------------------ items that were split, rows of the padding
 
-// grid: (items, blocks of rows of an item).  WPR wavefronts join a row: the slots of the item's spans in the order of the units
-// (of every WPR-th wavefront its own, then the wavefronts in their order).
-constexpr int kCombineThreads = 256;
-template <typename T, int D, int WPR>
-__global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(AttnParams p) {
-  constexpr int kWaves = kCombineThreads / 64, kRowsAtOnce = kWaves / WPR, E = D / 64;
-  constexpr int kRowsPerWg = WPR == 1 ? 4 : 1;
-  __shared__ float sX[WPR == 1 ? 1 : WPR][D], sL[WPR == 1 ? 1 : WPR];
-  const int item = blockIdx.x, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id();
-  const PairView w(p, item / p.tiles_per_pair);
-  const int r0 = item % p.tiles_per_pair * p.tm;
-  const int4 join = r0 < w.M ? p.joins[item] : int4{0, 0, 0, 0};       // an item without rows has no entry
-  const int w0 = __builtin_amdgcn_readfirstlane(join.x), w1 = __builtin_amdgcn_readfirstlane(join.y);
-  const int slot0 = __builtin_amdgcn_readfirstlane(join.z);
-  const int full = p.c.G * p.c.n_new;
-  for (int k = 0; k < kRowsPerWg; k += kRowsAtOnce) {
-    const int rl = blockIdx.y * kRowsPerWg + k + wave / WPR, r = r0 + rl;
-    if (rl >= p.tm || r >= full) break;                 // WPR > 1: all wavefronts alike
-    if (r < w.M && w0 == w1) continue;                   // one span had all of it and wrote the rows
-    long long at_lse;
-    T* dst = static_cast<T*>(p.O) + out_row(p, w, r, at_lse) + lane * E;
-    float m = -INFINITY, l = 0.f, x[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = 0.f;
-    if (r < w.M) {
-      auto slot_row = [&](int v) { return (long long)(v == w0 ? slot0 : 2 * v) * p.tm + rl; };
-      for (int v = w0 + lane; v <= w1; v += 64) m = fmaxf(m, p.part_ml[slot_row(v) * 2]);
-      m = wave_max(m);
-      const float ref = m == -INFINITY ? 0.f : m;
-      const int part = wave % WPR;
-#pragma unroll 8
-      for (int v = w0 + part; v <= w1; v += WPR) {
-        const long long row = slot_row(v);
-        const f32x2 ml = *reinterpret_cast<const f32x2*>(p.part_ml + row * 2);
-        const float wgt = fast_exp2(ml[0] - ref);
-        l = fmaf(ml[1], wgt, l);
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = fmaf(p.part_o[row * D + lane * E + e], wgt, x[e]);
-      }
-    }
-    if constexpr (WPR > 1) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) sX[wave][lane * E + e] = x[e];
-      if (lane == 0) sL[wave] = l;
-      __syncthreads();
-      if (wave != 0) return;                             // a workgroup has one row
-#pragma unroll
-      for (int v = 1; v < WPR; ++v) {
-        l += sL[v];
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] += sX[v][lane * E + e];
-      }
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) Elem<T>::store(dst + e, x[e] * inv);
-    if (lane == 0) p.lse[at_lse] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+// What the two kernels below share: the spans of an item, and where a row's part of a span lies.
+struct Join {
+  int w0, w1, slot0;
+  __device__ __forceinline__ Join(const AttnParams& p, const PairView& w, int item, int r0) {
+    const int4 j = r0 < w.M ? p.joins[item] : int4{0, 0, 0, 0};       // an item without rows has no entry
+    w0 = __builtin_amdgcn_readfirstlane(j.x);
+    w1 = __builtin_amdgcn_readfirstlane(j.y);
+    slot0 = __builtin_amdgcn_readfirstlane(j.z);
   }
+  __device__ __forceinline__ long long row(const AttnParams& p, int v, int rl) const { return (long long)(v == w0 ? slot0 : 2 * v) * p.tm + rl; }
+};
+
+constexpr int kCombineThreads = 256;
+
+// Items of 256 or 128 rows, shared by few spans: 16 lanes a row, four rows a wavefront.  grid: (items, blocks of 16 rows of an item)
+template <typename T, int D>
+__global__ __launch_bounds__(kCombineThreads) void paged_combine_rows_kernel(AttnParams p) {
+  constexpr int E = D / 16;
+  const int item = blockIdx.x, pair = item / p.tiles_per_pair, r0 = (item - pair * p.tiles_per_pair) * p.tm;
+  const PairView w = PairView::uniform(p, pair);
+  const Join join(p, w, item, r0);
+  const int rl = blockIdx.y * 16 + threadIdx.x / 16, r = r0 + rl, c = threadIdx.x % 16;
+  // one span had all of the item and wrote its rows; rows of the padding get zeros
+  if (rl >= p.tm || r >= p.c.G * p.c.n_new || (r < w.M && join.w0 == join.w1)) return;
+  long long at_lse;
+  T* dst = static_cast<T*>(p.O) + out_row(p, w, r, at_lse) + c * E;
+  float m = -INFINITY, l = 0.f, x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = 0.f;
+  if (r < w.M) {
+#pragma unroll 4
+    for (int v = join.w0; v <= join.w1; ++v) {           // running maximum: one pass, the loads of four parts at a time
+      const long long at = join.row(p, v, rl);
+      const f32x2 ml = *reinterpret_cast<const f32x2*>(p.part_ml + at * 2);
+      f32x4 y[E / 4];
+#pragma unroll
+      for (int k = 0; k < E / 4; ++k) y[k] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + c * E + 4 * k);
+      const float top = fmaxf(m, ml[0]), ref = top == -INFINITY ? 0.f : top;
+      const float old = fast_exp2(m - ref), add = fast_exp2(ml[0] - ref);
+      l = l * old + ml[1] * add;
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = x[e] * old + y[e / 4][e % 4] * add;
+      m = top;
+    }
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] *= inv;
+  if constexpr (sizeof(T) == 2 && E == 8) {
+    *reinterpret_cast<u32x4*>(dst) = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+  } else if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<u32x2*>(dst) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+  } else {
+#pragma unroll
+    for (int k = 0; k < E / 4; ++k) *reinterpret_cast<f32x4*>(dst + 4 * k) = f32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
+  }
+  if (c == 0) p.lse[at_lse] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+}
+
+// Items of up to 32 rows, shared by up to all spans: a workgroup a row, every fourth span a wavefront, the wavefronts in their order.
+// grid: (items, rows of an item)
+template <typename T, int D>
+__global__ __launch_bounds__(kCombineThreads) void paged_combine_spans_kernel(AttnParams p) {
+  constexpr int kWaves = kCombineThreads / 64, E = D / 64;
+  __shared__ float sX[kWaves][D], sL[kWaves];
+  const int item = blockIdx.x, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id();
+  const PairView w = PairView::uniform(p, item / p.tiles_per_pair);
+  const Join join(p, w, item, 0);                        // 32 rows: a pair is one item
+  const int r = blockIdx.y;
+  if (r < w.M && join.w0 == join.w1) return;
+  long long at_lse;
+  T* dst = static_cast<T*>(p.O) + out_row(p, w, r, at_lse) + lane * E;
+  float m = -INFINITY, l = 0.f, x[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = 0.f;
+  if (r < w.M) {
+    for (int v = join.w0 + lane; v <= join.w1; v += 64) m = fmaxf(m, p.part_ml[join.row(p, v, r) * 2]);
+    m = wave_max(m);
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll 8
+    for (int v = join.w0 + wave; v <= join.w1; v += kWaves) {
+      const long long at = join.row(p, v, r);
+      const f32x2 ml = *reinterpret_cast<const f32x2*>(p.part_ml + at * 2);
+      const float wgt = fast_exp2(ml[0] - ref);
+      l = fmaf(ml[1], wgt, l);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = fmaf(p.part_o[at * D + lane * E + e], wgt, x[e]);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) sX[wave][lane * E + e] = x[e];
+  if (lane == 0) sL[wave] = l;
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int v = 1; v < kWaves; ++v) {
+    l += sL[v];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] += sX[v][lane * E + e];
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) Elem<T>::store(dst + e, x[e] * inv);
+  if (lane == 0) p.lse[at_lse] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
 // ------------------------------------------------------------------ which kernel, how many workgroups
 
 struct Plan {
-  int tm, unit, n_wgs, min_share;
+  int tm, unit, over, n_wgs, min_share;
   bool logits;                                           // scores of the pass are kept for the weights
 };
 
 Plan make_plan(const Chunk& c, int dtype, int weight_rows) {
   const int rows = c.G * c.n_new;
   Plan pl;
-  if (rows <= 32) pl = Plan{32, 128, dtype == OMNI_BF16 && c.D == 64 ? 512 : 256, 1, false};
-  else pl = dtype == OMNI_BF16 ? Plan{256, 64, 256, 2, false} : Plan{128, 32, 512, 2, false};
+  if (rows <= 32) pl = Plan{32, 128, 0, dtype == OMNI_BF16 && c.D == 64 ? 512 : 256, 1, false};
+  else pl = dtype == OMNI_BF16 ? Plan{256, 64, 5, 256, 4, false} : Plan{128, 32, 1, 512, 2, false};
   pl.logits = weight_rows > 0 && dtype == OMNI_BF16 && pl.tm == 32;
   return pl;
 }
@@ -729,9 +775,9 @@ void carve(AttnParams& p, const Plan& pl, int dtype, int weight_rows, void* ws, 
 
 int launch_combine(const AttnParams& p, int dtype, hipStream_t st) {
   const int rows = min(p.tm, p.c.G * p.c.n_new);
-#define OMNI_COMBINE(T, D)                                                                                                       \
-  (p.tm == 32 ? paged_combine_kernel<T, D, 4><<<dim3(p.n_items, rows), kCombineThreads, 0, st>>>(p)                              \
-              : paged_combine_kernel<T, D, 1><<<dim3(p.n_items, cdiv(rows, 4)), kCombineThreads, 0, st>>>(p))
+#define OMNI_COMBINE(T, D)                                                                                          \
+  (p.tm == 32 ? paged_combine_spans_kernel<T, D><<<dim3(p.n_items, rows), kCombineThreads, 0, st>>>(p)              \
+              : paged_combine_rows_kernel<T, D><<<dim3(p.n_items, cdiv(rows, 16)), kCombineThreads, 0, st>>>(p))
   if (dtype == OMNI_BF16) {
     if (p.c.D == 128) OMNI_COMBINE(u16, 128);
     else OMNI_COMBINE(u16, 64);
@@ -762,6 +808,7 @@ int run_paged_attn(const Chunk& c, int dtype, const void* Q, const Pages& pg, co
   carve(p, pl, dtype, weight_rows, ws, nullptr);
   p.tm = pl.tm;
   p.unit = pl.unit;
+  p.over = pl.over;
   p.n_wgs = pl.n_wgs;
   p.min_share = pl.min_share;
   p.tiles_per_pair = cdiv(c.G * c.n_new, pl.tm);

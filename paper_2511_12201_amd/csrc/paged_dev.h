@@ -1,11 +1,12 @@
 // Device code that the attention kernels on a paged cache share: the rows of a pair, and how the work is cut.
 //
 // An item is up to tm consecutive query rows of a pair (sequence, KV head); it walks the cache rows that its last query row
-// sees, in units of `unit` rows.  All units of all items, item after item, are one line that is cut into as many equal spans as
+// sees, in units of `unit` rows, and counts `over` units more for what it costs to take it up (2048 tokens on as many rows: the
+// workgroup with the first, short items of a pair had six of them and took 97 us where the others took 50).  All units of all items, item after item, are one line that is cut into as many equal spans as
 // there are workgroups: every workgroup does the same amount of work whatever the lengths are, and the lengths stay on the
 // device.  A workgroup that has all units of an item writes its output rows; otherwise it leaves a partial state (maximum, sum,
 // weighted rows) in one of its two slots (its span's first item: slot 2 w, another one: it can only be the last: 2 w + 1), and
-// paged_combine_kernel joins the slots of an item in the order of the units: equal inputs, equal bits.  The workgroup that has an
+// the paged_combine kernels join the slots of an item in the order of the units: equal inputs, equal bits.  The workgroup that has an
 // item's first unit writes down which spans share it.
 #pragma once
 
@@ -27,6 +28,7 @@ struct AttnParams {
   float* acc_out;
   Chunk c;
   int tm, unit, tiles_per_pair, n_items;   // items: tiles_per_pair of every pair
+  int over;                                // units that stand for what taking up an item costs
   int n_wgs, min_share;                    // workgroups, units that a span has at least
   float* part_o;                           // [2 n_wgs, tm, D]
   float* part_ml;                          // [2 n_wgs, tm, 2]: maximum (times scale log2 e), sum
@@ -58,20 +60,37 @@ struct PairView {
   __device__ __forceinline__ int visible(const AttnParams& p, int t) const { return p.c.causal ? max(end - cnt + t + 1, 0) : end; }
 };
 
-__device__ __forceinline__ int item_units(const AttnParams& p, int item) {
-  const PairView w(p, item / p.tiles_per_pair);
-  const int r0 = item % p.tiles_per_pair * p.tm;
+// Units of an item that starts at query row r0: what the workgroup that takes a part of it pays besides the tiles, then the tiles.
+__device__ __forceinline__ int item_units(const AttnParams& p, const PairView& w, int r0) {
   if (r0 >= w.M) return 0;
   const int keys = w.visible(p, (min(r0 + p.tm, w.M) - 1) / p.c.G);
-  return max(1, cdiv(keys, p.unit));
+  return p.over + max(1, cdiv(keys, p.unit));
+}
+__device__ __forceinline__ int item_units(const AttnParams& p, int item) {
+  const int pair = item / p.tiles_per_pair;
+  return item_units(p, PairView(p, pair), (item - pair * p.tiles_per_pair) * p.tm);
 }
 
-// Spans of the line of units: workgroup w of n has [start(w), start(w + 1)).
+__device__ __forceinline__ u64 wave_uniform(u64 v) {
+  return ((u64)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+
+// Spans of the line of units: workgroup w of n has [start(w), start(w + 1)), the first total % n one unit more than the others.
 struct Spans {
-  u64 total;
+  u64 total, each, more;
   int n;
-  __device__ __forceinline__ u64 start(int w) const { return total * (u64)w / (u64)n; }
-  __device__ __forceinline__ int owner(u64 at) const { return (int)(((at + 1) * (u64)n + total - 1) / total) - 1; }
+  __device__ __forceinline__ void cut(u64 units, int wgs, int min_share) {
+    total = units = wave_uniform(units);
+    n = (int)max(1ull, min((u64)wgs, (units >> 32) == 0 ? (u64)((unsigned)units / (unsigned)min_share) : (u64)wgs));
+    each = (units >> 32) == 0 ? (u64)((unsigned)units / (unsigned)n) : units / n;
+    more = units - each * n;
+  }
+  __device__ __forceinline__ u64 start(int w) const { return each * w + min((u64)w, more); }
+  __device__ __forceinline__ int owner(u64 at) const {
+    const u64 long_ones = more * (each + 1);
+    if (total >> 32) return (int)(at < long_ones ? at / (each + 1) : more + (at - long_ones) / each);
+    return at < long_ones ? (int)((unsigned)at / (unsigned)(each + 1)) : (int)more + (int)((unsigned)(at - long_ones) / (unsigned)each);
+  }
 };
 
 struct Scan {
@@ -80,25 +99,10 @@ struct Scan {
   int item;
 };
 
-// Every thread: units of its run of consecutive items; returns the units in front of the run, total of all.
-template <int THREADS>
-__device__ __forceinline__ u64 scan_items(const AttnParams& p, Scan& s, int& first, int& per, u64& own, Spans& sp) {
-  per = cdiv(p.n_items, THREADS);
-  first = min((int)threadIdx.x * per, p.n_items);
-  own = 0;
-  for (int i = first; i < min(first + per, p.n_items); ++i) own += item_units(p, i);
-  const u64 inc = wave_scan(own);
-  if ((threadIdx.x & 63) == 63) s.wave[threadIdx.x >> 6] = inc;
-  __syncthreads();
-  u64 before = inc - own;
-  sp.total = 0;
-#pragma unroll
-  for (int v = 0; v < THREADS / 64; ++v) {
-    if (v < (int)(threadIdx.x >> 6)) before += s.wave[v];
-    sp.total += s.wave[v];
-  }
-  sp.n = (int)max(1ull, min((u64)p.n_wgs, sp.total / p.min_share));
-  return before;
+// Neighbouring spans go to one XCD (workgroup b runs on XCD b % 8): they share a pair, and often the place in it.
+__device__ __forceinline__ int span_of(int b, int n) {
+  const int each = n / 8;
+  return b < each * 8 ? b % 8 * each + b / 8 : b;
 }
 
 struct Segment {
@@ -106,49 +110,74 @@ struct Segment {
   bool whole;
 };
 
-// Walks a workgroup's span: f(segment) for its part of every item in it.  All threads call it.
-// Neighbouring spans go to one XCD (workgroup b runs on XCD b % 8): they share a pair, and often the place in it.
-__device__ __forceinline__ int span_of(int b, int n) {
-  const int each = n / 8;
-  return b < each * 8 ? b % 8 * each + b / 8 : b;
-}
-
+// Walks a workgroup's span: f(segment) for its part of every item in it.  All threads call it.  Up to 64 items (a few sequences of
+// few tokens, where the start counts) every wavefront finds its place by itself, one item a lane; more are added up by the workgroup.
 template <int THREADS, typename F>
 __device__ __forceinline__ void for_segments(const AttnParams& p, Scan& s, F f) {
-  int first, per;
-  u64 own;
   Spans sp;
-  u64 at = scan_items<THREADS>(p, s, first, per, own, sp);
-  if (sp.total == 0 || (int)blockIdx.x >= sp.n) return;
-  const int w = span_of(blockIdx.x, sp.n);
-  const u64 begin = sp.start(w), end = sp.start(w + 1);
-  if (begin >= at && begin < at + own) {
-    int i = first;
-    for (;; ++i) {
-      const int n = item_units(p, i);
-      if (begin < at + n) break;
-      at += n;
+  u64 begin, at_item;                                    // where the span begins, and its first item
+  int item, w;
+  if (p.n_items <= 64) {
+    const int mine = lane_id() < p.n_items ? item_units(p, lane_id()) : 0;
+    const u64 inc = wave_scan((u64)mine);
+    sp.cut(__shfl(inc, 63, 64), p.n_wgs, p.min_share);
+    if (sp.total == 0 || (int)blockIdx.x >= sp.n) return;
+    w = span_of(blockIdx.x, sp.n);
+    begin = sp.start(w);
+    item = __ffsll((unsigned long long)__ballot(inc > begin)) - 1;
+    at_item = __shfl(inc - mine, item, 64);
+  } else {
+    const int per = cdiv(p.n_items, THREADS), first = min((int)threadIdx.x * per, p.n_items);
+    u64 own = 0;
+    for (int i = first; i < min(first + per, p.n_items); ++i) own += item_units(p, i);
+    const u64 inc = wave_scan(own);
+    if ((threadIdx.x & 63) == 63) s.wave[threadIdx.x >> 6] = inc;
+    __syncthreads();
+    u64 at = inc - own, total = 0;
+#pragma unroll
+    for (int v = 0; v < THREADS / 64; ++v) {
+      if (v < (int)(threadIdx.x >> 6)) at += s.wave[v];
+      total += s.wave[v];
     }
-    s.item = i;
-    s.at = begin - at;
+    sp.cut(total, p.n_wgs, p.min_share);
+    if (sp.total == 0 || (int)blockIdx.x >= sp.n) return;
+    w = span_of(blockIdx.x, sp.n);
+    begin = sp.start(w);
+    if (begin >= at && begin < at + own) {
+      for (int i = first;; ++i) {
+        const int n = item_units(p, i);
+        if (begin < at + n) {
+          s.item = i;
+          s.at = at;
+          break;
+        }
+        at += n;
+      }
+    }
+    __syncthreads();
+    item = s.item;
+    at_item = s.at;
   }
-  __syncthreads();
-  int item = __builtin_amdgcn_readfirstlane(s.item), off = __builtin_amdgcn_readfirstlane((int)s.at);
+  const u64 end = sp.start(w + 1);
+  item = __builtin_amdgcn_readfirstlane(item);
+  int off = __builtin_amdgcn_readfirstlane((int)(begin - at_item));
   for (u64 pos = begin; pos < end; ++item) {
     const int units = __builtin_amdgcn_readfirstlane(item_units(p, item));
     if (units == 0) continue;
-    const int take = (int)min((u64)(units - off), end - pos);
+    const int take = (int)min((u64)(units - off), end - pos), tiles = units - p.over;
     Segment seg;
     seg.item = item;
     seg.pair = item / p.tiles_per_pair;
-    seg.r0 = item % p.tiles_per_pair * p.tm;
-    seg.u0 = off;
-    seg.u1 = off + take;
+    seg.r0 = (item - seg.pair * p.tiles_per_pair) * p.tm;
+    seg.u0 = max(off - p.over, 0);
+    seg.u1 = off + take - p.over;
     seg.slot = 2 * w + (pos == begin ? 0 : 1);
-    seg.whole = off == 0 && take == units;
-    if (off == 0 && threadIdx.x == 0)                    // who joins the item finds its slots here (whole: first span = last)
-      p.joins[item] = int4{w, seg.whole ? w : sp.owner(pos + units - 1), seg.slot, 0};
-    f(seg);
+    seg.whole = seg.u0 == 0 && seg.u1 == tiles;
+    if (seg.u1 > seg.u0) {
+      if (seg.u0 == 0 && threadIdx.x == 0)               // who joins the item finds its slots here (whole: first span = last)
+        p.joins[item] = int4{w, seg.whole ? w : sp.owner(pos + (units - off) - 1), seg.slot, 0};
+      f(seg);
+    }
     pos += take;
     off = 0;
   }

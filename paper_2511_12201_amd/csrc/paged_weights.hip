@@ -43,17 +43,15 @@ __device__ __forceinline__ void for_weight_segments(const AttnParams& p, Scan& s
   const u64 inc = wave_scan(own);
   if ((threadIdx.x & 63) == 63) s.wave[threadIdx.x >> 6] = inc;
   __syncthreads();
-  u64 at = inc - own;
-  Spans sp;
-  sp.total = 0;
+  u64 at = inc - own, total = 0;
 #pragma unroll
   for (int v = 0; v < THREADS / 64; ++v) {
     if (v < (int)(threadIdx.x >> 6)) at += s.wave[v];
-    sp.total += s.wave[v];
+    total += s.wave[v];
   }
-  if (sp.total == 0) return;
-  sp.n = (int)max(1ull, min((u64)gridDim.x, sp.total));
-  if ((int)blockIdx.x >= sp.n) return;
+  Spans sp;
+  sp.cut(total, gridDim.x, 1);
+  if (total == 0 || (int)blockIdx.x >= sp.n) return;
   const int w = span_of(blockIdx.x, sp.n);
   const u64 begin = sp.start(w), end = sp.start(w + 1);
   if (begin >= at && begin < at + own) {
@@ -69,7 +67,7 @@ __device__ __forceinline__ void for_weight_segments(const AttnParams& p, Scan& s
   }
   __syncthreads();
   int pair = __builtin_amdgcn_readfirstlane(s.item);
-  u64 off = ((u64)(unsigned)__builtin_amdgcn_readfirstlane((int)(s.at >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)s.at);
+  u64 off = wave_uniform(s.at);
   for (u64 pos = begin; pos < end; ++pair, off = 0) {
     const PairView view = PairView::uniform(p, pair);
     const PairBlocks pb(p, view, keys, rows);
