@@ -382,7 +382,7 @@ __global__ __launch_bounds__(kChunkThreads) void evict_lists_kernel(EvictParams 
       w.acc_out[j] = w.acc[j];
     }
     if (blockIdx.x == 0 && tid == 0) {
-      p.row_cnt[pair] = w.keep;
+      p.row_cnt[pair] = w.n;                             // the count as it was, cut to its range: a chunk that reads it later gets the same
       p.moves[pair] = 0;
     }
     return;
@@ -432,10 +432,7 @@ __global__ __launch_bounds__(kChunkThreads) void evict_lists_kernel(EvictParams 
       start[1] = h - h_own;
       start[2] = m - m_own;
     }
-    if (blockIdx.x == 0 && lane == 63) {
-      p.row_cnt[pair] = w.keep;
-      p.moves[pair] = m;
-    }
+    if (blockIdx.x == 0 && lane == 63) p.moves[pair] = m;
   }
   __syncthreads();
   int tie0 = start[0], place0 = begin < w.keep ? start[1] : start[2];
@@ -484,13 +481,14 @@ __global__ __launch_bounds__(kChunkThreads) void evict_lists_kernel(EvictParams 
   }
 }
 
-// The rows that change places.  grid: (blocks, pairs)
+// The rows that change places, and the new counts: row_cnt may be row_end, which the launches before read.  grid: (blocks, pairs)
 constexpr int kMoveThreads = 256;
 template <int LANES>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p) {
   const int pair = blockIdx.y;
   const PairRows w(p, pair);
   constexpr int kRows = kMoveThreads / LANES;
+  if (blockIdx.x == 0 && threadIdx.x == 0) p.row_cnt[pair] = w.keep;
   move_rows<LANES>(p, w, pair, p.moves[pair], blockIdx.x * kRows + threadIdx.x / LANES, gridDim.x * kRows, threadIdx.x % LANES);
 }
 

@@ -747,12 +747,15 @@ struct Plan {
   bool logits;                                           // scores of the pass are kept for the weights
 };
 
+// Pairs of at most 32 query rows stream the cache.  us a call, stream / tiles, 28 heads on 4: one token on 131089 rows 55 / 85, four
+// tokens on 4109 rows 14 / 22, on 131089 of eight sequences 391 / 405, with weights 654 / 721; 32 heads on 4 of 64 elements, four
+// tokens on 4109 rows 13.8 / 15.5, on 131089 of eight sequences 204 / 189.  Above, a stream would read the cache twice.
+// Workgroups: what the chip holds at once (LDS: one a CU, two of the streams and of the fp32 tiles with their small stages).
 Plan make_plan(const Chunk& c, int dtype, int weight_rows) {
-  const int rows = c.G * c.n_new;
-  Plan pl;
-  if (rows <= 32) pl = Plan{32, 128, 0, dtype == OMNI_BF16 && c.D == 64 ? 512 : 256, 1, false};
-  else pl = dtype == OMNI_BF16 ? Plan{256, 64, 5, 256, 4, false} : Plan{128, 32, 1, 512, 2, false};
-  pl.logits = weight_rows > 0 && dtype == OMNI_BF16 && pl.tm == 32;
+  const bool few = c.G * c.n_new <= kStreamRows, bf16 = dtype == OMNI_BF16;
+  Plan pl = few ? Plan{32, 128, 0, bf16 && c.D == 64 ? 512 : 256, 1, false}
+                : bf16 ? Plan{256, 64, 5, 256, 4, false} : Plan{128, 32, 1, 512, 2, false};
+  pl.logits = weight_rows > 0 && bf16 && few;
   return pl;
 }
 

@@ -113,90 +113,107 @@ __device__ __forceinline__ void put_weight(const AttnParams& p, const WeightSegm
   }
 }
 
-// fp32.  Weights from the finished log-sum-exps: a wavefront owns 32 cache rows, the query rows pass by.
+// fp32.  A wavefront keeps 32 cache rows as operands in registers; tiles of 32 query rows pass through LDS, the next one on its way in
+// registers.  The matrix instructions bound it (D / 2 of 64 cycles per 32 x 32 weights).
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_weights_f32_kernel(AttnParams p) {
-  __shared__ __attribute__((aligned(16))) float sQ[32 * (D + 4)];
+  constexpr int CPR = D / 4, NL = 32 * CPR / kThreads, PITCH = D + 4;
+  __shared__ __attribute__((aligned(16))) float sQ[32 * PITCH];
   __shared__ float sL[32];
   __shared__ int sVis[32];
   __shared__ Scan scan;
   const Chunk& c = p.c;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, ln = lane & 31, h = lane >> 5;
-  for_weight_segments<kThreads>(p, scan, kRows, 32, [&](const WeightSegment& seg, const PairView& w) {
-  const int j0 = seg.block * kRows + wave * 32;
-  const int row = j0 + ln < w.end ? pool_row(p.pg, w.pair, j0 + ln) : -1;
-  const unsigned there = (unsigned)__ballot(row >= 0) >> (4 * h);
-  float k[D / 2];
-#pragma unroll
-  for (int e = 0; e < D / 2; ++e) k[e] = 0.f;
-  if (row >= 0) {
-    const float* src = static_cast<const float*>(p.pg.K) + (long long)row * D + h * (D / 2);
-#pragma unroll
-    for (int e = 0; e < D / 2; e += 4) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(src + e);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) k[e + i] = x[i];
-    }
-  }
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = lane_id(), ln = lane & 31, h = lane >> 5;
   const float c2 = c.scale * kLog2e;
-  float sum[16];
+  for_weight_segments<kThreads>(p, scan, kRows, 32, [&](const WeightSegment& seg, const PairView& w) {
+    f32x4 next[NL];
+    float next_lse = -INFINITY;
+    int next_vis = 0;
+    auto load = [&](int r0) {                            // rows behind the last one as zeros, and nothing to see
+      long long at_lse;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-  constexpr int CPR = D / 4;
-  for (int r0 = seg.t0 * 32; r0 < seg.t1 * 32; r0 += 32) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < 32 * CPR; i += kThreads) {
-      const int r = r0 + i / CPR;
-      f32x4 x = {0.f, 0.f, 0.f, 0.f};
-      long long at_lse;
-      if (r < w.M) x = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.Q) + out_row(p, w, r, at_lse) + i % CPR * 4);
-      *reinterpret_cast<f32x4*>(sQ + (i / CPR) * (D + 4) + i % CPR * 4) = x;
-    }
-    if (threadIdx.x < 32) {
-      const int r = r0 + threadIdx.x;
-      float lse = -INFINITY;
-      long long at_lse;
-      if (r < w.M) {
-        out_row(p, w, r, at_lse);
-        lse = p.lse[at_lse];
+      for (int i = 0; i < NL; ++i) {
+        const int piece = i * kThreads + threadIdx.x, r = r0 + piece / CPR;
+        next[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (r < w.M) next[i] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.Q) + out_row(p, w, r, at_lse) + piece % CPR * 4);
       }
-      sL[threadIdx.x] = lse * kLog2e;
-      sVis[threadIdx.x] = lse > -INFINITY ? w.visible(p, r / c.G) : 0;
+      if (threadIdx.x < 32) {
+        const int r = r0 + threadIdx.x;
+        next_lse = -INFINITY;
+        if (r < w.M) {
+          out_row(p, w, r, at_lse);
+          next_lse = p.lse[at_lse];
+        }
+        next_vis = r < w.M ? w.visible(p, r / c.G) : 0;
+      }
+    };
+    load(seg.t0 * 32);
+    const int j0 = seg.block * kRows + wave * 32;
+    const int row = j0 + ln < w.end ? pool_row(p.pg, w.pair, j0 + ln) : -1;
+    const unsigned there = (unsigned)__ballot(row >= 0) >> (4 * h);
+    float k[D / 2];
+#pragma unroll
+    for (int e = 0; e < D / 2; ++e) k[e] = 0.f;
+    if (row >= 0) {
+      const float* src = static_cast<const float*>(p.pg.K) + (long long)row * D + h * (D / 2);
+#pragma unroll
+      for (int e = 0; e < D / 2; e += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(src + e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[e + i] = x[i];
+      }
     }
-    __syncthreads();
-    f32x16 s;
+    float sum[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+    for (int tile = seg.t0; tile < seg.t1; ++tile) {
+      __syncthreads();
 #pragma unroll
-    for (int e = 0; e < D / 2; e += 4) {
-      const f32x4 q = *reinterpret_cast<const f32x4*>(sQ + ln * (D + 4) + h * (D / 2) + e);
+      for (int i = 0; i < NL; ++i) {
+        const int piece = i * kThreads + threadIdx.x;
+        *reinterpret_cast<f32x4*>(sQ + piece / CPR * PITCH + piece % CPR * 4) = next[i];
+      }
+      if (threadIdx.x < 32) {
+        sL[threadIdx.x] = next_lse * kLog2e;
+        sVis[threadIdx.x] = next_lse > -INFINITY ? next_vis : 0;
+      }
+      __syncthreads();
+      if (tile + 1 < seg.t1) load((tile + 1) * 32);
+      f32x16 s;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e + x], q[x], s, 0, 0, 0);
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+      for (int e = 0; e < D / 2; e += 4) {
+        const f32x4 q = *reinterpret_cast<const f32x4*>(sQ + ln * PITCH + h * (D / 2) + e);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e + x], q[x], s, 0, 0, 0);
+      }
+      const int vis = sVis[ln];
+      const float ref = sL[ln];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = 8 * (i / 4) + i % 4;             // + 4 h
+        if (j0 + 4 * h + key < vis && ((there >> key) & 1u)) sum[i] += fast_exp2(fmaf(s[i], c2, -ref));
+      }
     }
-    const int vis = sVis[ln];
-    const float ref = sL[ln];
+    float own = 0.f;                                     // lane ln of a half takes the sum of register ln
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int key = 8 * (i / 4) + i % 4;
-      if (j0 + 4 * h + key < vis && ((there >> key) & 1u)) sum[i] += fast_exp2(fmaf(s[i], c2, -ref));
+      const float v = half_lanes_sum(sum[i]);
+      own = ln == i ? v : own;
     }
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    float v = sum[i];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    const int j = j0 + 8 * (i / 4) + 4 * h + i % 4;
-    if (ln == 0 && j < w.end) put_weight(p, seg, kRows, j - seg.block * kRows, j, v);
-  }
+    const int in_block = wave * 32 + 8 * (ln / 4) + 4 * h + ln % 4, j = seg.block * kRows + in_block;
+    if (ln < 16 && j < w.end) put_weight(p, seg, kRows, in_block, j, own);
   });
 }
 
 // bf16, many query rows.  A wavefront keeps 64 cache rows as fragments in registers and its sums per lane half; tiles of 64 query
-// rows go from memory straight into a ring of four LDS stages, three on their way while one is worked on, one barrier a tile.  (One
-// tile ahead through registers the loads' latency was the time of a tile: 238 us / W_US for 500 new tokens in four sequences of 8200
-// to 16400 rows.)  The scores of 32 query rows are formed under the weights of the 32 before: per 64 x 32 weights a wavefront
-// issues 16 matrix instructions (512 cycles) and 32 times scale, 2^x and sum (about 600).
+// rows go from memory straight into a ring of four LDS stages, three on their way while one is worked on, one barrier a tile.  The
+// scores of 32 query rows are formed under the weights of the 32 before: per 64 x 32 weights a wavefront issues 16 matrix
+// instructions (512 cycles) and 32 times scale, 2^x and sum (950 cycles with the four that each 2^x takes): the vector ALU bounds it.
+// 500 new tokens in four sequences of 8200 to 16400 rows: 190 us, 114 if nothing but those instructions counted; the rest is what a
+// block of cache rows costs to take up (11 us of the 65 us that its tiles take) and the second workgroup of a CU, which works alone
+// once the first, older one is through.
 constexpr int kBfKeys = 64, kBfRows = kWaves * kBfKeys, kBfQ = 64, kBfStages = 4;
 template <int D>
 __global__ __launch_bounds__(kThreads, 2) void paged_weights_bf16_kernel(AttnParams p) {
