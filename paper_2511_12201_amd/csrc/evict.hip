@@ -283,7 +283,7 @@ __device__ __forceinline__ void load_total(const EvictParams& p, int d, int pair
     i32x4 s = {0, 0, 0, 0};
     if (d == 0) {
       const int* src = chunk_hist(p, 0, pair, 0) + i;
-#pragma unroll 8
+#pragma unroll 20
       for (int c = 0; c < kChunks; ++c) s += *reinterpret_cast<const i32x4*>(src + c * kBins);
     } else {
       s = *reinterpret_cast<const i32x4*>(pair_total(p, d, pair) + i);
@@ -403,19 +403,27 @@ __global__ __launch_bounds__(kChunkThreads) void evict_lists_kernel(EvictParams 
   const unsigned cut = with_digit((unsigned)p.cut[pair * 4 + 2], f.bin, 2);
   const int need = f.left;
   // rows above the cut and ties of every chunk: a wavefront takes every kWaves-th chunk (the last digit has 1024 bins)
-  for (int c = wave; c < kChunks; c += kWaves) {
-    const int* h = chunk_hist(p, 2, pair, c);
-    int n = 0;
+  constexpr int kOwn = kChunks / kWaves;
+  static_assert(kOwn * kWaves == kChunks, "");
+  int higher[kOwn], equal[kOwn];
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) {                       // all loads first
+    const int* h = chunk_hist(p, 2, pair, wave + k * kWaves);
+    higher[k] = 0;
 #pragma unroll
     for (int i = lane * 4; i < 1024; i += 256) {
       const i32x4 x = *reinterpret_cast<const i32x4*>(h + i);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) n += i + e > f.bin ? x[e] : 0;
+      for (int e = 0; e < 4; ++e) higher[k] += i + e > f.bin ? x[e] : 0;
     }
-    n = wave_sum(n);
+    equal[k] = h[f.bin];
+  }
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) {
+    const int c = wave + k * kWaves, n = (int)__shfl(wave_scan((unsigned)higher[k]), 63, 64);
     if (lane == 0) {
       above[c] = n + p.above[pair * kChunks + c];
-      ties[c] = h[f.bin];
+      ties[c] = equal[k];
     }
   }
   __syncthreads();

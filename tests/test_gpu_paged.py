@@ -614,6 +614,44 @@ def test_two_streams_at_once_and_a_stream_that_is_not_the_default():
             assert torch.equal(a, b)
 
 
+class Guarded(ob.Workspace):
+    """Scratch of exactly the size that is asked for, with a pattern behind it."""
+
+    def get(self, call_id, desc, param=0):
+        need = ob.workspace_bytes(call_id, desc, param)
+        self.whole = torch.full((need + 4096,), 0xAB, dtype=torch.uint8, device="cuda")
+        return self.whole[:need]
+
+    def check(self):
+        assert (self.whole[-4096:] == 0xAB).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,end", [(1, 4000), (4, 700), (5, 100), (40, 3000), (300, 301)])
+def test_calls_stay_inside_their_scratch_and_outputs(dtype, n, end):
+    rng = np.random.default_rng(n)
+    B, H, Hkv, D = 2, 14, 2, 64
+    cache = Cache(rng, B, Hkv, -(-end // 16), 16, D, dtype)
+    Q = rand(rng, B, H, n, D, dtype=dtype)
+    desc, ws = ob.make_chunk_desc(Q, n_kv_heads=Hkv), Guarded()
+    rows = B * H * n
+    O, lse, acc = (torch.full((size + 256,), 7.0, dtype=dt, device="cuda") for size, dt in
+                   ((rows * D, dtype), (rows, F32), (B * Hkv * cache.cap, F32)))
+    ob.omni_paged_attn(desc, Q, cache.pool, ints([[end] * Hkv] * B), ints([n] * B), O=O[:-256].view(Q.shape), lse=lse[:-256].view(B, H, n),
+                       acc_out=acc[:-256].view(B, Hkv, cache.cap), ws=ws)
+    ws.check()
+    assert all((x[-256:] == 7.0).all() for x in (O, lse, acc))
+
+
+@pytest.mark.parametrize("pages", [3, 64, 200, 1030])
+def test_eviction_stays_inside_its_scratch(pages):
+    rng = np.random.default_rng(pages)
+    cache, ws = Cache(rng, 2, 2, pages, 16, 64, BF16), Guarded()
+    acc, pos = torch.rand(2, 2, cache.cap, device="cuda"), torch.zeros(2, 2, cache.cap, dtype=torch.int32, device="cuda")
+    ob.omni_paged_evict(cache.pool, cache.cap // 2, 0, 0, ints([5, 5]), ints([[cache.cap] * 2] * 2), pos, acc, ws=ws)
+    ws.check()
+
+
 def test_results_repeat_to_the_bit():
     rng = np.random.default_rng(12)
     cache = Cache(rng, 1, 2, 40, 64, 128, BF16)
