@@ -53,7 +53,7 @@ struct PairRows {
     cap = rows_cap(p.pg);
     n = clampi(p.row_end[pair], 0, cap);
     keep = min(n, p.budget);
-    recent = p.seq_len[pair / p.Hkv] - p.n_recent;
+    recent = (int)std::max((long long)p.seq_len[pair / p.Hkv] - p.n_recent, -(1ll << 31));
     n_sink = p.n_sink;
     const long long at = (long long)pair * cap;
     pos = p.row_pos + at;

@@ -6,8 +6,8 @@
 // Running maximum and sum, one pass over the rows.  Rows that are not there (behind the last one, or on a page that is missing)
 // enter as zeros and are masked.
 //
-//  * Few query rows a pair (paged_stream_kernel, at most 32): memory bounds it.  A wavefront takes 32 cache rows per trip, K
-//    straight from memory in fragment layout, V through a tile of its own that is read back transposed; no barrier in the loop.
+//  * Few query rows a pair (paged_stream_kernel, at most 32): memory bounds it.  Every wavefront streams 32-row blocks of the
+//    cache of its own through LDS; the states of a workgroup's wavefronts meet at an item's end.
 //  * Many (paged_tile_kernel): eight wavefronts of 32 query rows share 64-row tiles that go from the pages straight into a ring
 //    of four LDS stages, one barrier a tile; the softmax of a tile runs under the matrix instructions of the next.
 // The weights are rounded to bf16 for the second product (half a step: 2^-8 relative each, the errors of many rows average out);
@@ -26,8 +26,10 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // A wavefront takes 32 cache rows per trip, K and V straight from the pages into a ring of two LDS stages of its own: while one is
 // worked on the other is on its way, 64 to 128 KB per CU in flight, and no barrier in the loop.  (Loads through registers, three
-// workgroups a CU, kept less in flight: 131k rows of eight sequences took 567 us, KEEP_US now.)  An instruction takes 1024 bytes, whole
-// rows of one page; the pieces of a row change places as in the tile kernel below.  Blocks that are not whole go through registers.
+// workgroups a CU, kept less in flight: 131k rows of eight sequences and four KV heads of 128 elements, a token each, took 567 us
+// with the weights, 468 now; 378 without them, 5.7 TB/s where a copy, which also writes, reaches 5.1.)  An instruction takes 1024
+// bytes, whole rows of one page; the pieces of a row change places as in the tile kernel below.  Blocks that are not whole go through
+// registers.
 constexpr int kStreamWaves = 4, kStreamThreads = kStreamWaves * 64, kStreamRows = 32;
 
 // where the 16-byte pieces of row r of a tile lie: piece c at c ^ swz(r)
@@ -96,7 +98,7 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
           const long long row = (long long)(i * RPI < 16 ? row_a : row_b) + i * RPI % 16;
           gload_lds16(pool + row * RB, kIsK ? src_k[i % NP] : src_v, own_ring + at + i * 1024);
         }
-      } else {                                           // zeros for what is not there; these loads end here, and so do all before
+      } else {                                           // zeros for what is not there
 #pragma unroll
         for (int i = 0; i < LPH; ++i) {
           const int r = i * RPI + in_row, from = r < 16 ? row_a : row_b;
@@ -104,6 +106,8 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
           if (from >= 0 && block * 32 + r < w.end) x = *reinterpret_cast<const u32x4*>(pool + ((long long)from + r % 16) * RB + slot * 16);
           *reinterpret_cast<u32x4*>(own_bytes + at + r * RB + (slot ^ (kIsK ? swz_k<D>(r) : swz_v<D>(r))) * 16) = x;
         }
+        // every copy before ends here: a half that took no load of its own would be missing in the counts of the waits
+        wait_vmcnt<0>();
       }
     };
     constexpr std::true_type kKeys{};
@@ -256,12 +260,12 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
     float total = 0.f;
 #pragma unroll
     for (int v = 0; v < kStreamWaves; ++v) total = fmaf(sL[v][n], fast_exp2(sM[v][n] - ref), total);
-    const float inv = total > 0.f ? 1.f / total : 0.f;
+    const float inv = total == 0.f ? 0.f : 1.f / total;                 // a NaN among the scores stays one
     if (wave == 0 && h == 0 && n < w.M) {
       if (seg.whole) {
         long long at_lse;
         out_row(p, w, n, at_lse);
-        p.lse[at_lse] = total > 0.f ? (top + log2f(total)) * kLn2 : -INFINITY;
+        p.lse[at_lse] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
       } else {
         *reinterpret_cast<f32x2*>(p.part_ml + ((long long)seg.slot * kStreamRows + n) * 2) = f32x2{top, total};
       }
@@ -409,7 +413,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
         else gload_lds16(Vpool + row * RB, src_v, dst + kKBytes + at * 1024);
       };
       auto row_there = [&](int j) { return j < w.end ? sTab[(j >> p.pg.shift) - tab0] : -1; };
-      auto copy_tile = [&](int t) {                      // a tile that is not whole; its loads end here
+      auto copy_tile = [&](int t) {                      // a tile that is not whole; every load before ends here, as the counts of the waits assume
         unsigned char* dst = smem + (t % kStages) * kStageBytes;
         for (int i = threadIdx.x; i < kTileKeys * CPR; i += kTileThreads) {
           const int row = i / CPR, piece = i % CPR, j = (c0 + t) * kTileKeys + row;
@@ -423,6 +427,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
           *reinterpret_cast<u32x4*>(dst + row * RB + (piece ^ swz_k<D>(row)) * 16) = k;
           *reinterpret_cast<u32x4*>(dst + kKBytes + row * RB + (piece ^ swz_v<D>(row)) * 16) = v;
         }
+        wait_vmcnt<0>();
       };
       auto issue_tile = [&](int t) {
         if (t < n_plain) {
@@ -605,7 +610,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
     if (row_out >= w.M) return;
     long long at_lse;
     const long long at_row = out_row(p, w, row_out, at_lse);
-    const float by = !seg.whole ? 1.f : total > 0.f ? 1.f / total : 0.f;
+    const float by = !seg.whole ? 1.f : total == 0.f ? 0.f : 1.f / total;
     const long long at_part = (long long)seg.slot * kTileRows + row_out - seg.r0;
 #pragma unroll
     for (int db = 0; db < NB; ++db)
@@ -619,7 +624,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
           *reinterpret_cast<f32x4*>(p.part_o + at_part * D + d) = x;
       }
     if (h == 0) {
-      if (seg.whole) p.lse[at_lse] = total > 0.f ? (m_run * c2 + log2f(total)) * kLn2 : -INFINITY;
+      if (seg.whole) p.lse[at_lse] = total == 0.f ? -INFINITY : (m_run * c2 + log2f(total)) * kLn2;
       else *reinterpret_cast<f32x2*>(p.part_ml + at_part * 2) = f32x2{m_run * c2, total};
     }
   });
@@ -679,7 +684,7 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_rows_kernel(Att
       m = top;
     }
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int e = 0; e < E; ++e) x[e] *= inv;
   if constexpr (sizeof(T) == 2 && E == 8) {
@@ -690,7 +695,7 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_rows_kernel(Att
 #pragma unroll
     for (int k = 0; k < E / 4; ++k) *reinterpret_cast<f32x4*>(dst + 4 * k) = f32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
   }
-  if (c == 0) p.lse[at_lse] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  if (c == 0) p.lse[at_lse] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // Items of up to 32 rows, shared by up to all spans: a workgroup a row, every fourth span a wavefront, the wavefronts in their order.
@@ -734,10 +739,10 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_spans_kernel(At
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] += sX[v][lane * E + e];
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int e = 0; e < E; ++e) Elem<T>::store(dst + e, x[e] * inv);
-  if (lane == 0) p.lse[at_lse] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  if (lane == 0) p.lse[at_lse] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // ------------------------------------------------------------------ which kernel, how many workgroups

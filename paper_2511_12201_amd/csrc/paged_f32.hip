@@ -163,14 +163,14 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 1 : 2) void paged_attn_f32_kernel
     }
     if (!real) return;
     if (seg.whole) {
-      const float inv = total > 0.f ? 1.f / total : 0.f;
+      const float inv = total == 0.f ? 0.f : 1.f / total;
       float* dst = static_cast<float*>(p.O) + at_row;
 #pragma unroll
       for (int db = 0; db < NB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
           *reinterpret_cast<f32x4*>(dst + db * 32 + 2 * i + 4 * h) = f32x4{o[db][i] * inv, o[db][i + 1] * inv, o[db][i + 2] * inv, o[db][i + 3] * inv};
-      if (h == 0) p.lse[at_lse] = total > 0.f ? (m + log2f(total)) * kLn2 : -INFINITY;
+      if (h == 0) p.lse[at_lse] = total == 0.f ? -INFINITY : (m + log2f(total)) * kLn2;
     } else {
       const long long at = (long long)seg.slot * p.tm + r - seg.r0;
 #pragma unroll

@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kThreads) void paged_weights_f32_kernel(AttnParams 
       }
       if (threadIdx.x < 32) {
         sL[threadIdx.x] = next_lse * kLog2e;
-        sVis[threadIdx.x] = next_lse > -INFINITY ? next_vis : 0;
+        sVis[threadIdx.x] = next_lse == -INFINITY ? 0 : next_vis;
       }
       __syncthreads();
       if (tile + 1 < seg.t1) load((tile + 1) * 32);
@@ -323,9 +323,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_weights_bf16_kernel(AttnPar
       __builtin_amdgcn_sched_barrier(0);
       const float lse = sLse[stage][wave][qb * 32 + ln];
       ref = lse * kLog2e;
-      if ((tile + 1) * kBfQ > w.M || lse == -INFINITY) {          // behind the last row, or a row that sees nothing: 2^(x - inf) = 0
+      if ((tile + 1) * kBfQ > w.M || lse == -INFINITY) {          // behind the last row, or a row that sees nothing
         const int r = tile * kBfQ + qb * 32 + ln;
-        if (r >= w.M || lse == -INFINITY) ref = INFINITY;
+        if (r >= w.M || lse == -INFINITY) {
+          ref = 0.f;
+#pragma unroll
+          for (int x = 0; x < 32; ++x) s[x / 16][x % 16] = -INFINITY;
+        }
       }
       if (tile < clear) {
         const int rel = w.visible(p, (tile * kBfQ + qb * 32 + ln) / c.G) - j0 - 4 * h;
@@ -412,7 +416,7 @@ __global__ __launch_bounds__(kThreads) void paged_weights_logits_kernel(AttnPara
     if ((int)threadIdx.x < w.M) {
       out_row(p, w, threadIdx.x, at_lse);
       const float lse = p.lse[at_lse];
-      if (lse > -INFINITY) ref = lse * kLog2e;
+      if (lse != -INFINITY) ref = lse * kLog2e;
     }
     sL[threadIdx.x] = ref;
   }

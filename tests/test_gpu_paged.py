@@ -321,6 +321,30 @@ def test_pages_that_are_not_there(dtype, n):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [1, 5, 40, 300])
+def test_a_nan_stays_with_the_tokens_that_see_it(dtype, n):
+    rng = np.random.default_rng(n)
+    cache = Cache(rng, 2, 1, 30, 16, 64, dtype)
+    Q = rand(rng, 2, 3, n, 64, dtype=dtype)
+    desc, ends, cnt = ob.make_chunk_desc(Q, n_kv_heads=1), ints([[430], [460]]), ints([n, n])
+    outs = []
+    row = max(430 - 2, 430 - n)                               # the last one or two tokens see it
+    for value in (None, float("nan")):
+        if value is not None:
+            cache.K[cache.table[0, 0, row // 16].long(), row % 16, 5] = value
+        acc = torch.zeros(2, 1, cache.cap, device="cuda")
+        outs.append((*ob.omni_paged_attn(desc, Q, cache.pool, ends, cnt, acc_out=acc), acc))
+    (O, lse, acc), (bad_O, bad_lse, bad_acc) = outs
+    clean = row - (430 - n)
+    # rows of a wavefront may take another reference value: weights (2^-8 at most) and outputs are rounded anew; sums of 430 rows
+    assert not ((O - bad_O)[0, :, :clean].abs() > 4 * 2.0 ** -8 * cache.V.abs().max()).any() and torch.isfinite(bad_O[0, :, :clean]).all()
+    assert ((lse - bad_lse)[0, :, :clean].abs() <= 2 * (2 * 430 * U32 + 2.0 ** -20 + 4 * U32 * 64)).all()
+    assert bad_O[0, :, clean:].isnan().all() and bad_lse[0, :, clean:].isnan().all() and bad_acc[0, 0, :row + 1].isnan().all()
+    for x, y in ((O, bad_O), (lse, bad_lse), (acc, bad_acc)):
+        assert torch.equal(x[1], y[1])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_large_scores_and_equal_scores(dtype):
     """One row that takes everything, all rows alike, and scores that rise from tile to tile."""
     rng = np.random.default_rng(8)
@@ -489,6 +513,21 @@ def test_eviction_of_long_caches(pages, rows, budget, kind):
     pos = torch.arange(cache.cap, device="cuda").int().expand(2, 1, -1).contiguous()
     sink, recent = min(4, budget - 1), min(64, max(0, budget - 5))
     check_eviction(cache, budget, sink, recent, [rows, rows // 2], [[rows], [rows // 2 + 1]], pos, torch.from_numpy(acc).cuda())
+
+
+@pytest.mark.parametrize("pages", [8, 1100])
+def test_eviction_at_the_ends_of_the_range_of_positions(pages):
+    rng = np.random.default_rng(pages)
+    cache = Cache(rng, 1, 1, pages, 16, 64, BF16)
+    pos = torch.full((1, 1, cache.cap), 5, dtype=torch.int32, device="cuda")
+    pos[0, 0, 40], pos[0, 0, 41] = -2 ** 31, 2 ** 31 - 1
+    acc = torch.zeros(1, 1, cache.cap, device="cuda")
+    acc[0, 0, 50:60] = 1
+    for seq_len, rows in ((-2 ** 31, range(20)),              # every position is recent: the first rows stay
+                          (2 ** 31 - 1, [40, 41, *range(50, 60), *range(8)])):
+        _, got, weights = ob.omni_paged_evict(cache.pool, 20, 1, 19, ints([seq_len]), ints([[cache.cap - 3]]), pos, acc)
+        assert sorted(got[0, 0, :20].tolist()) == sorted(pos[0, 0, list(rows)].tolist())
+        assert weights[0, 0, :20].sum().item() == acc[0, 0, list(rows)].sum().item()
 
 
 def test_eviction_where_more_rows_are_spared_than_fit_and_pages_are_missing():
