@@ -1,15 +1,18 @@
 // Eviction from a paged cache by accumulated attention weight (omni_paged_evict).
 //
 // Per (sequence, KV head) pair the rows are ranked by a 32-bit key (spared rows above every weight, the weights in order, NaN
-// below them) and the `keep` largest stay, equal keys by lowest row.  The key at the cut is found digit by digit (11, 11 and 10
-// bits) with histograms in LDS; then the rows are counted in order, which splits the ties and numbers the holes and the rows that
-// move into them.  Rows are only copied where they have to: a row that stays in front of the new end stays where it is.
+// below them) and the `keep` largest stay, equal keys by lowest row.  The key at the cut is found by histograms in LDS of 11 bits
+// of the keys at a time; then the rows are counted in order, which splits the ties and numbers the holes and the rows that move into
+// them.  Rows are only copied where they have to: a row that stays in front of the new end stays where it is.
 //
 // The selection has to read 8 bytes a row, the moves 4 rows' bytes each; what bounds a small call is the chain of dependent steps.
 //  * Up to 16384 rows a pair (evict_small_kernel): one workgroup a pair, its keys in registers throughout, one launch and one for
-//    the moves; where a pair can have few moves the workgroup makes them itself and the second launch is left out.
+//    the moves; where a pair can have few moves the workgroup makes them itself and the second launch is left out.  16 of 8192 rows,
+//    32 pairs: 9.5 us, of which 2 are the rows' loads and 1.3 the moves (three fixed digits, rows in the order of the threads and
+//    what is counted in that order by ballots: 14).
 //  * More: the pair's rows in front of the new end and those behind it are cut into chunks, a workgroup each: three launches for
-//    the digits (every chunk leaves its histogram, the next launch adds them up), one for the lists, one for the moves.
+//    the digits (every chunk leaves its histogram, the next launch finds the bin), one for the lists, one for the moves.  98304 of
+//    131072 rows leave, 8 pairs: 5.2 + 6.4 + 6.1 + 10.2 + 39 us, the last at the rate of a copy.
 #include <algorithm>
 
 #include "paged.h"
@@ -20,6 +23,7 @@ namespace {
 
 constexpr int kSmallRows = 16384, kSmallThreads = 1024;
 constexpr int kFewMoves = 256;                 // moves that the workgroup of a pair makes itself
+constexpr int kRanked = 128;                   // keys of a bin that are compared with one another instead of counted by digits
 constexpr int kBins = 2048;
 constexpr int kChunks = 40, kChunkThreads = 512, kChunkRows = 8;     // 38 whole chunks of at most 4096 rows: 155k rows in one round
 
@@ -32,7 +36,7 @@ struct EvictParams {
   float* acc_out;
   int* moves;                    // [pairs]
   int2* list;                    // [pairs, cap / 2] (from, to)
-  int *hist, *total, *above;     // many rows: [3][pairs, kChunks, kBins], [2][pairs, kBins], [pairs, kChunks]
+  int *hist, *coarse, *above;    // many rows: [3][pairs, kChunks, kBins], [3][pairs, kChunks, 64], [pairs, kChunks]
   int* cut;                      // [pairs, 4] digits found and rows wanted of the last one
 };
 
@@ -74,39 +78,49 @@ __device__ __forceinline__ unsigned with_digit(unsigned prefix, int bin, int d) 
 __device__ __forceinline__ void count_key(int* hist, int bin, bool counts) {
   const unsigned long long who = __ballot(counts);
   if (who == 0) return;
-  const int first = __shfl(bin, __ffsll((unsigned long long)who) - 1, 64);
-  if (__all(!counts || bin == first)) {
+  const int first = __builtin_amdgcn_readlane(bin, __ffsll(who) - 1);
+  if (__ballot(counts && bin != first) == 0) {
     if (lane_id() == 0) atomicAdd(&hist[first], __popcll(who));
   } else if (counts) {
     atomicAdd(&hist[bin], 1);
   }
 }
 
-// The bin that holds the need-th largest key, how many of it are wanted, and whether that is all of it; hist in LDS, all threads
-// call it.
+// Largest of the wavefront's values, in every lane.
+__device__ __forceinline__ unsigned wave_umax(unsigned v) {
+  v = max(v, dpp_or_zero<0x111, 0xf>(v));
+  v = max(v, dpp_or_zero<0x112, 0xf>(v));
+  v = max(v, dpp_or_zero<0x114, 0xf>(v));
+  v = max(v, dpp_or_zero<0x118, 0xf>(v));
+  v = max(v, dpp_or_zero<0x142, 0xa>(v));
+  v = max(v, dpp_or_zero<0x143, 0xc>(v));
+  return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+// The bin that holds the need-th largest key, how many of it are wanted, and how many it holds.
 struct Found {
-  int bin, left, all;
+  int bin, left, count;
 };
-template <int THREADS>
+// From a histogram in LDS; all threads of evict_small_kernel call it.
 __device__ __forceinline__ Found find_bin(const int* hist, int need, int* wave_sums, int* out) {
-  constexpr int PER = kBins / THREADS, kWaves = THREADS / 64;
+  constexpr int PER = kBins / kSmallThreads, kWaves = kSmallThreads / 64;
   int own = 0, h[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     h[i] = hist[kBins - 1 - ((int)threadIdx.x * PER + i)];       // from the largest key down
     own += h[i];
   }
-  const int inc = (int)wave_scan((unsigned)own), wave = threadIdx.x >> 6;
+  const int inc = (int)wave_scan((unsigned)own), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   if (lane_id() == 63) wave_sums[wave] = inc;
   __syncthreads();
   const int sums = (int)wave_scan((unsigned)(lane_id() < kWaves ? wave_sums[lane_id()] : 0));
-  int before = inc - own + (wave ? __shfl(sums, wave - 1, 64) : 0);
+  int before = inc - own + (wave ? __builtin_amdgcn_readlane(sums, wave - 1) : 0);
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     if (before < need && need <= before + h[i]) {
       out[0] = kBins - 1 - ((int)threadIdx.x * PER + i);
       out[1] = need - before;
-      out[2] = need == before + h[i];
+      out[2] = h[i];
     }
     before += h[i];
   }
@@ -115,11 +129,11 @@ __device__ __forceinline__ Found find_bin(const int* hist, int need, int* wave_s
 }
 
 // K and V of moved rows and what they carry; LANES lanes a row.
-template <int LANES>
-__device__ __forceinline__ void move_rows(const EvictParams& p, const PairRows& w, int pair, int moves, int first, int step, int lane) {
+template <int LANES, typename LIST>
+__device__ __forceinline__ void move_rows(const EvictParams& p, const PairRows& w, const LIST& list, int pair, int moves, int first, int step, int lane) {
   const int per = p.row_bytes / 16;
   for (int i = first; i < moves; i += step) {
-    const int2 m = w.list[i];
+    const int2 m = list[i];
     if (lane == 0) {
       w.pos_out[m.y] = w.pos[m.x];                       // rows behind `keep` are never written: in place is as good
       w.acc_out[m.y] = w.acc[m.x];
@@ -136,129 +150,192 @@ __device__ __forceinline__ void move_rows(const EvictParams& p, const PairRows& 
 
 // ------------------------------------------------------------------ up to kSmallRows rows a pair.  grid: pairs
 
-// R rows a thread: row k * kSmallThreads + thread.
+typedef int i32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// Sum of the values in front of a thread's, and of all; all threads of evict_small_kernel call it.
+struct Before {
+  unsigned before, all;
+};
+__device__ __forceinline__ Before scan_threads(unsigned v, int wave, unsigned* sums) {
+  constexpr int kWaves = kSmallThreads / 64;
+  const unsigned inc = wave_scan(v);
+  if (lane_id() == 63) sums[wave] = inc;
+  __syncthreads();
+  const int s = (int)wave_scan(lane_id() < kWaves ? sums[lane_id()] : 0u);
+  return Before{inc - v + (wave ? (unsigned)__builtin_amdgcn_readlane(s, wave - 1) : 0u), (unsigned)__builtin_amdgcn_readlane(s, kWaves - 1)};
+}
+
+// R neighbouring rows a thread: what has to be counted in the order of the rows are bits of one register, and one sum over the threads.
 template <int R>
 __global__ __launch_bounds__(kSmallThreads) void evict_small_kernel(EvictParams p) {
-  constexpr int kWaves = kSmallThreads / 64, kCells = R * kWaves, CPL = kCells / 64;   // cells (k, wavefront) in the order of the rows
   __shared__ int hist[3][kBins];
-  __shared__ int sums[kWaves], out[3];
-  __shared__ __attribute__((aligned(16))) unsigned cell[2][kCells];
-  const int pair = blockIdx.x, tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
+  __shared__ int sums[kSmallThreads / 64], out[3];
+  __shared__ unsigned tie_sums[kSmallThreads / 64], move_sums[kSmallThreads / 64];
+  __shared__ int2 few[kFewMoves];                        // the list of the moves, where the workgroup makes them itself
+  __shared__ unsigned long long cand[kRanked], bound;
+  __shared__ int n_cand;
+  __shared__ unsigned ends[2][2];                        // of the keys of a bin: the largest, and of their complements
+  const int pair = blockIdx.x, tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const PairRows w(p, pair);
+  const int j0 = tid * R;
+  auto bits = [&](int rows) { return (1u << clampi(rows - j0, 0, R)) - 1; };
+  const unsigned live = bits(w.n), front = bits(w.keep);
   unsigned key[R];
   int pos[R];
   float acc[R];
 #pragma unroll
-  for (int k = 0; k < R; ++k) {
-    const int j = k * kSmallThreads + tid;
-    pos[k] = j < w.n ? w.pos[j] : 0;
-    acc[k] = j < w.n ? w.acc[j] : 0.f;
-  }
-  int movers = 0;
-  if (w.keep < w.n) {
-    for (int i = tid; i < 3 * kBins; i += kSmallThreads) hist[0][i] = 0;
+  for (int k = 0; k < R; k += 4) {
+    if (j0 + k + 4 <= w.n) {
+      const i32x4_4 q = *reinterpret_cast<const i32x4_4*>(w.pos + j0 + k);
+      const f32x4_4 a = *reinterpret_cast<const f32x4_4*>(w.acc + j0 + k);
 #pragma unroll
-    for (int k = 0; k < R; ++k) key[k] = w.key(acc[k], pos[k]);
-    unsigned cut = 0;
-    int need = w.keep;
-    __syncthreads();
-    for (int d = 0; d < 3; ++d) {
-#pragma unroll
-      for (int k = 0; k < R; ++k) {
-        if (k * kSmallThreads + wave * 64 < w.n)         // wave-uniform
-          count_key(hist[d], digit_of(key[k], d), k * kSmallThreads + tid < w.n && same_above(key[k], cut, d));
+      for (int e = 0; e < 4; ++e) {
+        pos[k + e] = q[e];
+        acc[k + e] = a[e];
       }
-      __syncthreads();
-      const Found f = find_bin<kSmallThreads>(hist[d], need, sums, out);
-      cut = with_digit(cut, f.bin, d);
-      need = f.left;
-      if (f.all) {                                       // every key from here on stays, whatever its other digits
-        need = 0x7fffffff;
-        break;
-      }
-    }
-    // in front of a thread's cell k: the counts of the cells before; 16 bits each for two kinds (a pair has at most 16384 rows)
-    unsigned base[CPL];
-    auto scan_cells = [&](const unsigned* c) {
-      unsigned sum = 0;
-#pragma unroll
-      for (int i = 0; i < CPL; ++i) {
-        base[i] = sum;
-        sum += c[lane * CPL + i];
-      }
-      const unsigned before = wave_scan(sum) - sum;
-#pragma unroll
-      for (int i = 0; i < CPL; ++i) base[i] += before;
-    };
-    auto before_cell = [&](int k) {
-      unsigned v = base[0];                              // cell k * kWaves + wave is piece wave % CPL of lane (k * kWaves + wave) / CPL
-#pragma unroll
-      for (int i = 1; i < CPL; ++i) v = wave % CPL == i ? base[i] : v;
-      return __shfl(v, (k * kWaves + wave) / CPL, 64);
-    };
-    const unsigned long long below = (1ull << lane) - 1;
-    unsigned stay = 0;
-    if (need == 0x7fffffff) {
-#pragma unroll
-      for (int k = 0; k < R; ++k)
-        if (k * kSmallThreads + tid < w.n && key[k] >= cut) stay |= 1u << k;
     } else {
 #pragma unroll
-      for (int k = 0; k < R; ++k) {
-        const unsigned long long b = __ballot(k * kSmallThreads + tid < w.n && key[k] == cut);
-        if (lane == 0) cell[0][k * kWaves + wave] = __popcll(b);
+      for (int e = 0; e < 4; ++e) {
+        pos[k + e] = live >> (k + e) & 1u ? w.pos[j0 + k + e] : 0;
+        acc[k + e] = live >> (k + e) & 1u ? w.acc[j0 + k + e] : 0.f;
+      }
+    }
+  }
+  for (int i = tid; i < 3 * kBins; i += kSmallThreads) hist[0][i] = 0;
+  if (tid < 4) ends[tid / 2][tid % 2] = 0;
+  if (tid == 0) n_cand = 0;
+#pragma unroll
+  for (int k = 0; k < R; ++k) asm volatile("" : "+v"(pos[k]), "+v"(acc[k]));     // loaded here: later waits would be for the stores, too
+  // what the rows of `rows` in front of the new end carry
+  auto keep_rows = [&](unsigned rows) {
+#pragma unroll
+    for (int k = 0; k < R; k += 4) {
+      if ((rows >> k & 15u) == 15u) {
+        *reinterpret_cast<i32x4_4*>(w.pos_out + j0 + k) = i32x4_4{pos[k], pos[k + 1], pos[k + 2], pos[k + 3]};
+        *reinterpret_cast<f32x4_4*>(w.acc_out + j0 + k) = f32x4_4{acc[k], acc[k + 1], acc[k + 2], acc[k + 3]};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (rows >> (k + e) & 1u) {
+            w.pos_out[j0 + k + e] = pos[k + e];
+            w.acc_out[j0 + k + e] = acc[k + e];
+          }
+      }
+    }
+  };
+  int movers = 0;
+  unsigned kept = live;
+  if (w.keep < w.n) {
+#pragma unroll
+    for (int k = 0; k < R; ++k) key[k] = w.key(acc[k], pos[k]);
+    // Level by level: the keys of [base, base + span] by their bits from `low` on, at most 11; then the bin that holds the cut is
+    // the range, narrowed to what it holds.
+    unsigned base_key = 0, span = ~0u;
+    int low = 21, need = w.keep;
+    bool ties = false;                                   // many equal keys base_key at the cut; else a row stays if ranked >= least
+    unsigned long long least = 0;
+    auto ranked = [&](int k) { return (unsigned long long)key[k] << 32 | ~(unsigned)(j0 + k); };
+    auto inside = [&](int k) { return (live >> k & 1u) && key[k] - base_key <= span; };
+    __syncthreads();
+    for (int level = 0;; ++level) {                      // 21, at most 10, 0
+      if (wave * 64 * R < w.n) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) count_key(hist[level], (int)((key[k] - base_key) >> low), inside(k));
       }
       __syncthreads();
-      scan_cells(cell[0]);
+      const Found f = find_bin(hist[level], need, sums, out);
+      base_key = (unsigned)__builtin_amdgcn_readfirstlane((int)(base_key + ((unsigned)f.bin << low)));
+      span = (1u << low) - 1;
+      need = __builtin_amdgcn_readfirstlane(f.left);
+      const int count = __builtin_amdgcn_readfirstlane(f.count);
+      if (count == need) {                               // all of them stay
+        least = (unsigned long long)base_key << 32;
+        break;
+      }
+      if (count <= kRanked) {                            // few: the last to stay is the one that need - 1 of them are larger than
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+          if (inside(k)) cand[atomicAdd(&n_cand, 1)] = ranked(k);
+        __syncthreads();
+        constexpr int kParts = kSmallThreads / kRanked;
+        const int i = tid / kParts;
+        const unsigned long long own = i < count ? cand[i] : 0;
+        int larger = 0;
+        for (int c = tid % kParts; c < count; c += kParts) larger += cand[c] > own;
+#pragma unroll
+        for (int o = kParts / 2; o > 0; o >>= 1) larger += __shfl_xor(larger, o, 64);
+        if (tid % kParts == 0 && i < count && larger == need - 1) bound = own;
+        __syncthreads();
+        least = bound;
+        break;
+      }
+      ties = low == 0;
+      if (ties) break;
+      unsigned top = 0, bottom = 0;
 #pragma unroll
       for (int k = 0; k < R; ++k) {
-        const int j = k * kSmallThreads + tid;
-        const bool tie = j < w.n && key[k] == cut;
-        const unsigned long long b = __ballot(tie);
-        const int before = (int)before_cell(k) + __popcll(b & below);
-        if (j < w.n && (key[k] > cut || (tie && before < need))) stay |= 1u << k;
+        const bool in = inside(k);
+        top = max(top, in ? key[k] : 0u);
+        bottom = max(bottom, in ? ~key[k] : 0u);
+      }
+      top = wave_umax(top);
+      bottom = wave_umax(bottom);
+      if (lane == 0) {
+        atomicMax(&ends[level][0], top);
+        atomicMax(&ends[level][1], bottom);
+      }
+      __syncthreads();
+      base_key = (unsigned)__builtin_amdgcn_readfirstlane((int)~ends[level][1]);
+      span = (unsigned)__builtin_amdgcn_readfirstlane((int)ends[level][0]) - base_key;
+      ties = span == 0;
+      if (ties) break;
+      low = max(0, 21 - __builtin_clz(span));
+    }
+    unsigned stay = 0;
+    if (!ties) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) stay |= ranked(k) >= least ? 1u << k : 0u;
+    } else {
+      unsigned tie = 0;
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        stay |= key[k] > base_key ? 1u << k : 0u;
+        tie |= key[k] == base_key ? 1u << k : 0u;
+      }
+      tie &= live;
+      int more = need - (int)scan_threads(__popc(tie), wave, tie_sums).before;
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        const unsigned one = tie & 1u << k;
+        stay |= more > 0 ? one : 0u;
+        more -= one != 0;
       }
     }
+    stay &= live;
+    const unsigned hole = front & ~stay, mover = stay & ~front;
+    // 16 bits each: a pair has at most 16384 rows
+    const Before b = scan_threads(__popc(hole) | __popc(mover) << 16, wave, move_sums);
+    movers = (int)(b.all >> 16);
+    auto list_rows = [&](int2* list) {
+      int at_hole = (int)(b.before & 0xffffu), at_mover = (int)(b.before >> 16);
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-      const int j = k * kSmallThreads + tid;
-      const bool s = stay >> k & 1u;
-      const unsigned long long bh = __ballot(j < w.keep && !s), bm = __ballot(j >= w.keep && s);
-      if (lane == 0) cell[1][k * kWaves + wave] = (unsigned)__popcll(bh) | (unsigned)__popcll(bm) << 16;
-    }
+      for (int k = 0; k < R; ++k) {
+        if (hole >> k & 1u) list[at_hole++].y = j0 + k;
+        if (mover >> k & 1u) list[at_mover++].x = j0 + k;
+      }
+    };
+    if (p.move_here) list_rows(few);
+    else list_rows(w.list);
+    kept = stay & front;
     __syncthreads();
-    scan_cells(cell[1]);
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      const int j = k * kSmallThreads + tid;
-      const bool s = stay >> k & 1u, hole = j < w.keep && !s, mover = j >= w.keep && s;
-      const unsigned long long bh = __ballot(hole), bm = __ballot(mover);
-      const unsigned before = before_cell(k);
-      if (hole) w.list[(before & 0xffffu) + __popcll(bh & below)].y = j;
-      if (mover) w.list[(before >> 16) + __popcll(bm & below)].x = j;
-      if (j < w.keep && s) {
-        w.pos_out[j] = pos[k];
-        w.acc_out[j] = acc[k];
-      }
-      if (k == R - 1 && wave == kWaves - 1 && lane == 0) out[0] = (int)(before >> 16) + __popcll(bm);
-    }
-    __syncthreads();
-    movers = out[0];
-  } else {
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      const int j = k * kSmallThreads + tid;
-      if (j < w.n) {
-        w.pos_out[j] = pos[k];
-        w.acc_out[j] = acc[k];
-      }
-    }
   }
   if (tid == 0) {
     p.row_cnt[pair] = w.keep;
     p.moves[pair] = movers;
   }
-  if (p.move_here) move_rows<16>(p, w, pair, movers, tid / 16, kSmallThreads / 16, tid % 16);
+  if (p.move_here) move_rows<16>(p, w, few, pair, movers, tid / 16, kSmallThreads / 16, tid % 16);
+  keep_rows(kept);                                       // last: nothing waits for these stores
 }
 
 // ------------------------------------------------------------------ more rows.  grid: (kChunks, pairs)
@@ -271,34 +348,76 @@ __device__ __forceinline__ void chunk_rows(const PairRows& w, int c, int& begin,
   end = max(begin, end);
 }
 
-// One entry of `hist` per (digit, pair, chunk, bin), of `total` per (digit 1 or 2, pair, bin), of `above` per (pair, chunk).
+// One entry of `hist` per (digit, pair, chunk, bin), of `coarse` per (digit, pair, chunk, 32 bins), of `above` per (pair, chunk).
+constexpr int kFine = kBins / 64;
 __device__ __forceinline__ int* chunk_hist(const EvictParams& p, int d, int pair, int c) {
   return p.hist + (((long long)d * gridDim.y + pair) * kChunks + c) * kBins;
 }
-__device__ __forceinline__ int* pair_total(const EvictParams& p, int d, int pair) { return p.total + ((long long)(d - 1) * gridDim.y + pair) * kBins; }
-
-// Digit d of all chunks of the pair into LDS: the chunks' histograms added up (digit 0), or what they have added to the pair's.
-__device__ __forceinline__ void load_total(const EvictParams& p, int d, int pair, int* hist) {
-  for (int i = threadIdx.x * 4; i < kBins; i += kChunkThreads * 4) {
-    i32x4 s = {0, 0, 0, 0};
-    if (d == 0) {
-      const int* src = chunk_hist(p, 0, pair, 0) + i;
-#pragma unroll 20
-      for (int c = 0; c < kChunks; ++c) s += *reinterpret_cast<const i32x4*>(src + c * kBins);
-    } else {
-      s = *reinterpret_cast<const i32x4*>(pair_total(p, d, pair) + i);
-    }
-    *reinterpret_cast<i32x4*>(hist + i) = s;
-  }
-  __syncthreads();
+__device__ __forceinline__ int* chunk_coarse(const EvictParams& p, int d, int pair, int c) {
+  return p.coarse + (((long long)d * gridDim.y + pair) * kChunks + c) * 64;
 }
 
-// Histogram of digit D among the keys that share the digits found so far.  Digit 0 also clears the pair's totals of the other two.
+// The bin of digit d that holds the need-th largest key, how many of it are wanted, and whether that is all of it, from the chunks'
+// histograms: the 32 bins first that hold it, then the bin.  (All bins of all chunks are 320 KB a workgroup: 12.5 us for a launch of
+// 320 workgroups that takes 6 so.)  Wavefront v reads chunks v, v + 8, .. and keeps their counts: with them it knows how many keys of
+// such a chunk lie above the bin.  All threads call `find`.
+struct DigitCut {
+  static constexpr int kWaves = kChunkThreads / 64, kOwn = kChunks / kWaves;
+  static_assert(kOwn * kWaves == kChunks && kFine == 32, "");
+  int wide[kOwn], fine[(kOwn + 1) / 2];                  // fine: chunk k of the wavefront in lanes 32 (k % 2) .. + 31
+  Found f;
+  __device__ __forceinline__ void find(const EvictParams& p, int d, int pair, int need, int (*part)[64]) {
+    const int lane = lane_id(), wave = threadIdx.x >> 6;
+    int s = 0;
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) wide[k] = chunk_coarse(p, d, pair, wave + k * kWaves)[lane];
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) s += wide[k];
+    part[wave][lane] = s;
+    __syncthreads();
+    // a lane a bin, the largest first: the lane in which the keys so far reach `need`
+    int n = 0;
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) n += part[v][63 - lane];
+    int inc = (int)wave_scan((unsigned)n);
+    int at = __ffsll((unsigned long long)__ballot(inc >= need)) - 1;
+    const int group = 63 - at;
+    need -= __shfl(inc - n, at, 64);
+    s = 0;
+#pragma unroll
+    for (int k = 0; k < (kOwn + 1) / 2; ++k) {
+      const int own = 2 * k + lane / 32;
+      fine[k] = own < kOwn ? chunk_hist(p, d, pair, wave + own * kWaves)[group * kFine + lane % 32] : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < (kOwn + 1) / 2; ++k) s += fine[k];
+    __syncthreads();                                     // everyone has read `part`
+    part[wave][lane] = s;
+    __syncthreads();
+    n = 0;
+#pragma unroll
+    for (int v = 0; v < 2 * kWaves; ++v) n += part[v / 2][v % 2 * 32 + 31 - lane % 32];
+    if (lane >= 32) n = 0;
+    inc = (int)wave_scan((unsigned)n);
+    at = __ffsll((unsigned long long)__ballot(inc >= need)) - 1;
+    const int all = __shfl(n, at, 64);
+    f.left = need - __shfl(inc - n, at, 64);
+    f.bin = group * kFine + 31 - at;
+    f.count = all;
+  }
+  // keys above the bin of the wavefront's chunk k, and in it
+  __device__ __forceinline__ int2 chunk(int k) const {
+    const int lane = lane_id(), at = f.bin % kFine;
+    const int n = (lane > f.bin / kFine ? wide[k] : 0) + (lane / 32 == k % 2 && lane % 32 > at ? fine[k / 2] : 0);
+    return int2{(int)__shfl(wave_scan((unsigned)n), 63, 64), __shfl(fine[k / 2], k % 2 * 32 + at, 64)};
+  }
+};
+
+// Histogram of digit D among the keys that share the digits found so far.
 template <int D>
 __global__ __launch_bounds__(kChunkThreads) void evict_digit_kernel(EvictParams p) {
-  constexpr int kWaves = kChunkThreads / 64;
   __shared__ __attribute__((aligned(16))) int hist[kBins];
-  __shared__ int sums[kWaves], out[3];
+  __shared__ int part[kChunkThreads / 64][64];
   const int pair = blockIdx.y, tid = threadIdx.x;
   const PairRows w(p, pair);
   if (w.keep == w.n) return;
@@ -319,27 +438,20 @@ __global__ __launch_bounds__(kChunkThreads) void evict_digit_kernel(EvictParams 
   if constexpr (D > 0) {
     const int need = D == 1 ? w.keep : p.cut[pair * 4 + 1];
     prefix = D == 1 ? 0u : (unsigned)p.cut[pair * 4];
-    load_total(p, D - 1, pair, hist);
-    const Found f = find_bin<kChunkThreads>(hist, need, sums, out);
-    prefix = with_digit(prefix, f.bin, D - 1);
+    const int so_far = D == 1 ? 0 : p.above[pair * kChunks + blockIdx.x];
+    DigitCut digit;
+    digit.find(p, D - 1, pair, need, part);
+    prefix = with_digit(prefix, digit.f.bin, D - 1);
     if (blockIdx.x == 0 && tid == 0) {                   // for the next launch; digits of different launches do not meet
       p.cut[pair * 4 + (D == 1 ? 0 : 2)] = (int)prefix;
-      p.cut[pair * 4 + (D == 1 ? 1 : 3)] = f.left;
+      p.cut[pair * 4 + (D == 1 ? 1 : 3)] = digit.f.left;
     }
-    // keys of this chunk above the bin
-    const int* own = chunk_hist(p, D - 1, pair, blockIdx.x);
-    int n = 0;
-    for (int i = tid; i < kBins; i += kChunkThreads) n += i > f.bin ? own[i] : 0;
-    n = wave_sum(n);
-    if (lane_id() == 0) sums[tid >> 6] = n;
-    __syncthreads();
-    if (tid == 0) {
-      n = D == 1 ? 0 : p.above[pair * kChunks + blockIdx.x];
-      for (int v = 0; v < kWaves; ++v) n += sums[v];
-      p.above[pair * kChunks + blockIdx.x] = n;
+#pragma unroll
+    for (int k = 0; k < DigitCut::kOwn; ++k) {           // keys of this chunk above the bin
+      if (tid / 64 + k * DigitCut::kWaves != (int)blockIdx.x) continue;
+      const int n = digit.chunk(k).x;
+      if (lane_id() == 0) p.above[pair * kChunks + blockIdx.x] = so_far + n;
     }
-  } else if (blockIdx.x == 0) {
-    for (int i = tid; i < kBins; i += kChunkThreads) pair_total(p, 1, pair)[i] = pair_total(p, 2, pair)[i] = 0;
   }
   for (int i = tid; i < kBins; i += kChunkThreads) hist[i] = 0;
   __syncthreads();
@@ -352,16 +464,11 @@ __global__ __launch_bounds__(kChunkThreads) void evict_digit_kernel(EvictParams 
     }
   }
   __syncthreads();
-  int* dst = chunk_hist(p, D, pair, blockIdx.x);
-  for (int i = tid * 4; i < kBins; i += kChunkThreads * 4) {
-    const i32x4 h = *reinterpret_cast<const i32x4*>(hist + i);
-    *reinterpret_cast<i32x4*>(dst + i) = h;
-    if constexpr (D > 0) {                               // integers: the order of the additions does not matter
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (h[e]) atomicAdd(pair_total(p, D, pair) + i + e, h[e]);
-    }
-  }
+  static_assert(kBins == 4 * kChunkThreads, "four bins a thread, 32 of 8 lanes");
+  const i32x4 h = *reinterpret_cast<const i32x4*>(hist + tid * 4);
+  *reinterpret_cast<i32x4*>(chunk_hist(p, D, pair, blockIdx.x) + tid * 4) = h;
+  const int n = (int)wave_scan((unsigned)(h[0] + h[1] + h[2] + h[3])), before = __shfl(n, (tid & 56) - 1, 64);
+  if (tid % 8 == 7) chunk_coarse(p, D, pair, blockIdx.x)[tid / 8] = n - ((tid & 63) > 7 ? before : 0);
 }
 
 // Lists of holes and movers, and what the rows that stay carry.  A chunk's first places follow from the histograms: the rows of
@@ -369,8 +476,7 @@ __global__ __launch_bounds__(kChunkThreads) void evict_digit_kernel(EvictParams 
 __global__ __launch_bounds__(kChunkThreads) void evict_lists_kernel(EvictParams p) {
   constexpr int kWaves = kChunkThreads / 64, R = kChunkRows, kRound = R * kChunkThreads;
   static_assert(R * kWaves == 64, "a lane a cell");
-  __shared__ __attribute__((aligned(16))) int hist[kBins];
-  __shared__ int sums[kWaves], out[3], above[kChunks], ties[kChunks], start[3];
+  __shared__ int part[kWaves][64], above[kChunks], ties[kChunks], start[3];
   __shared__ unsigned cell[2][64];
   const int pair = blockIdx.y, tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
   const PairRows w(p, pair);
@@ -398,32 +504,19 @@ __global__ __launch_bounds__(kChunkThreads) void evict_lists_kernel(EvictParams 
     }
   };
   load(begin);
-  load_total(p, 2, pair, hist);
-  const Found f = find_bin<kChunkThreads>(hist, p.cut[pair * 4 + 3], sums, out);
-  const unsigned cut = with_digit((unsigned)p.cut[pair * 4 + 2], f.bin, 2);
-  const int need = f.left;
-  // rows above the cut and ties of every chunk: a wavefront takes every kWaves-th chunk (the last digit has 1024 bins)
-  constexpr int kOwn = kChunks / kWaves;
-  static_assert(kOwn * kWaves == kChunks, "");
-  int higher[kOwn], equal[kOwn];
+  int higher[DigitCut::kOwn];                            // rows above the digits before, of the wavefront's chunks
 #pragma unroll
-  for (int k = 0; k < kOwn; ++k) {                       // all loads first
-    const int* h = chunk_hist(p, 2, pair, wave + k * kWaves);
-    higher[k] = 0;
+  for (int k = 0; k < DigitCut::kOwn; ++k) higher[k] = p.above[pair * kChunks + wave + k * kWaves];
+  DigitCut digit;
+  digit.find(p, 2, pair, p.cut[pair * 4 + 3], part);
+  const unsigned cut = with_digit((unsigned)p.cut[pair * 4 + 2], digit.f.bin, 2);
+  const int need = digit.f.left;
 #pragma unroll
-    for (int i = lane * 4; i < 1024; i += 256) {
-      const i32x4 x = *reinterpret_cast<const i32x4*>(h + i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) higher[k] += i + e > f.bin ? x[e] : 0;
-    }
-    equal[k] = h[f.bin];
-  }
-#pragma unroll
-  for (int k = 0; k < kOwn; ++k) {
-    const int c = wave + k * kWaves, n = (int)__shfl(wave_scan((unsigned)higher[k]), 63, 64);
+  for (int k = 0; k < DigitCut::kOwn; ++k) {
+    const int2 n = digit.chunk(k);
     if (lane == 0) {
-      above[c] = n + p.above[pair * kChunks + c];
-      ties[c] = equal[k];
+      above[wave + k * kWaves] = n.x + higher[k];
+      ties[wave + k * kWaves] = n.y;
     }
   }
   __syncthreads();
@@ -448,6 +541,8 @@ __global__ __launch_bounds__(kChunkThreads) void evict_lists_kernel(EvictParams 
   const unsigned long long below = (1ull << lane) - 1;
   for (int j0 = begin; j0 < end; j0 += kRound) {
     if (j0 != begin) load(j0);
+#pragma unroll
+    for (int k = 0; k < R; ++k) asm volatile("" : "+v"(pos[k]), "+v"(acc[k]));   // loaded here: later waits would be for the stores, too
     unsigned long long tie[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
@@ -497,7 +592,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictParams p)
   const PairRows w(p, pair);
   constexpr int kRows = kMoveThreads / LANES;
   if (blockIdx.x == 0 && threadIdx.x == 0) p.row_cnt[pair] = w.keep;
-  move_rows<LANES>(p, w, pair, p.moves[pair], blockIdx.x * kRows + threadIdx.x / LANES, gridDim.x * kRows, threadIdx.x % LANES);
+  move_rows<LANES>(p, w, w.list, pair, p.moves[pair], blockIdx.x * kRows + threadIdx.x / LANES, gridDim.x * kRows, threadIdx.x % LANES);
 }
 
 void carve(EvictParams& p, int pairs, int cap, Arena& a) {
@@ -506,7 +601,7 @@ void carve(EvictParams& p, int pairs, int cap, Arena& a) {
   if (cap > kSmallRows) {
     p.cut = a.take<int>((size_t)pairs * 4);
     p.hist = a.take<int>((size_t)3 * pairs * kChunks * kBins);
-    p.total = a.take<int>((size_t)2 * pairs * kBins);
+    p.coarse = a.take<int>((size_t)3 * pairs * kChunks * 64);
     p.above = a.take<int>((size_t)pairs * kChunks);
   }
 }

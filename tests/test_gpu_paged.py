@@ -503,6 +503,20 @@ def test_eviction_with_equal_and_odd_weights(rows, budget, kind):
     check_eviction(cache, budget, 0, 0, [cache.cap + 1], [[rows, rows - 1]], pos, torch.from_numpy(acc).cuda(), True)
 
 
+@pytest.mark.parametrize("rows", [900, 3001, 8190, 16383, 17000])
+@pytest.mark.parametrize("near", [1, 700, 5000, 1 << 21])
+def test_eviction_between_weights_that_are_close(rows, near):
+    """`near` neighbouring floats from 1 on, zeros and a few others: cuts in every third of a key, among many equal keys and few."""
+    rng = np.random.default_rng(rows + near)
+    cache = Cache(rng, 1, 1, -(-rows // 64), 64, 64, BF16)
+    acc = (np.float32(1.0).view(np.int32) + rng.integers(0, near, cache.cap).astype(np.int32)).view(np.float32)
+    other = rng.random(cache.cap)
+    acc = np.where(other < 0.1, np.float32(0.0), np.where(other > 0.99, np.float32(50.0) + other.astype(np.float32), acc))[None, None]
+    pos = torch.arange(cache.cap, device="cuda").int()[None, None]
+    for budget in (1, rows // 200 + 1, rows // 2, rows - rows // 10 + 3, rows - 1):
+        check_eviction(cache, budget, 0, 0, [cache.cap + 1], [[rows]], pos.clone(), torch.from_numpy(acc).cuda(), budget % 2 == 0)
+
+
 @pytest.mark.parametrize("pages,rows,budget", [(256, 16384, 16383), (256, 16000, 4000), (257, 16448, 100), (257, 300, 299), (257, 0, 5),
                                                (2000, 128000, 32000), (2000, 127999, 127998), (64, 4096, 1), (65, 4097, 4000)])
 @pytest.mark.parametrize("kind", ["weights", "zeros"])
