@@ -73,11 +73,11 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
   const unsigned char* qlane = sQ + n * QP + h * 16;
 
   for_segments<kStreamThreads>(p, scan, [&](const Segment& seg) {
-    const PairView w = PairView::uniform(p, seg.pair);
+    const PairView w = seg.w;
     const int keys = w.visible(p, (w.M - 1) / c.G);
     const int first = seg.u0 * kStreamWaves + wave, last = min(seg.u1 * kStreamWaves, cdiv(keys, 32));
     // read only while the kernel runs: entries come through the scalar cache, so that no wait for them is one for the copies
-    const auto* table = (const __attribute__((address_space(4))) int*)(p.pg.table + (long long)seg.pair * p.pg.pages_cap);
+    const auto* table = (const __attribute__((address_space(4))) int*)(p.pg.table + (long long)w.pair * p.pg.pages_cap);
     const int page_mask = (1 << p.pg.shift) - 1;
     // table entries of a block's two halves of 16 rows (each inside one page), and the pool row of a half, -1: not there
     auto entry = [&](int block, int half) {
@@ -92,14 +92,22 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
       constexpr bool kIsK = decltype(is_k)::value;
       const unsigned char* pool = kIsK ? Kpool : Vpool;
       const int at = stage * kStageBytes + (kIsK ? 0 : kKBytes);
-      if (row_a >= 0 && row_b >= 0 && block * 32 + 32 <= w.end) {
+      const int last_row = w.end - 1 - block * 32;       // of the block
+      if (__builtin_expect(row_a >= 0 && row_b >= 0 && last_row >= 31, true)) {
 #pragma unroll
         for (int i = 0; i < LPH; ++i) {
           const long long row = (long long)(i * RPI < 16 ? row_a : row_b) + i * RPI % 16;
           gload_lds16(pool + row * RB, kIsK ? src_k[i % NP] : src_v, own_ring + at + i * 1024);
         }
-      } else {                                           // zeros for what is not there
+      } else if (row_a >= 0 && (row_b >= 0 || last_row < 16)) {          // the last rows: behind the last one it again, which is masked
 #pragma unroll
+        for (int i = 0; i < LPH; ++i) {
+          const int r = min(i * RPI + in_row, last_row);
+          const unsigned piece = (kIsK ? src_k[i % NP] : src_v) - in_row * RB;
+          gload_lds16(pool + ((long long)(r < 16 ? row_a : row_b) + r % 16) * RB + piece, own_ring + at + i * 1024);
+        }
+      } else {                                           // pages that are not there: zeros
+#pragma unroll 1
         for (int i = 0; i < LPH; ++i) {
           const int r = i * RPI + in_row, from = r < 16 ? row_a : row_b;
           u32x4 x = {0u, 0u, 0u, 0u};
@@ -280,20 +288,17 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
       for (int i = 0; i < 16; i += 4)
         *reinterpret_cast<f32x4*>(sO + db * kGroup + (wave * 32 + n) * OP + 2 * i + 4 * h) = f32x4{o[db][i] * by, o[db][i + 1] * by, o[db][i + 2] * by, o[db][i + 3] * by};
     __syncthreads();
+    for (int i = threadIdx.x; i < w.M * (D / 4); i += kStreamThreads) {
+      const int r = i / (D / 4), d = i % (D / 4) * 4, at = d / 32 * kGroup + r * OP + d % 32;
+      f32x4 x = *reinterpret_cast<const f32x4*>(sO + at);
 #pragma unroll
-    for (int db = 0; db < NB; ++db) {
-      const int r = threadIdx.x / 8, d = threadIdx.x % 8 * 4;
-      if (r < w.M) {
-        f32x4 x = *reinterpret_cast<const f32x4*>(sO + db * kGroup + r * OP + d);
-#pragma unroll
-        for (int v = 1; v < kStreamWaves; ++v) x += *reinterpret_cast<const f32x4*>(sO + db * kGroup + (v * 32 + r) * OP + d);
-        if (seg.whole) {
-          long long at_lse;
-          u16* dst = static_cast<u16*>(p.O) + out_row(p, w, r, at_lse) + db * 32 + d;
-          *reinterpret_cast<uint2*>(dst) = uint2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
-        } else {
-          *reinterpret_cast<f32x4*>(p.part_o + ((long long)seg.slot * kStreamRows + r) * D + db * 32 + d) = x;
-        }
+      for (int v = 1; v < kStreamWaves; ++v) x += *reinterpret_cast<const f32x4*>(sO + at + v * 32 * OP);
+      if (seg.whole) {
+        long long at_lse;
+        u16* dst = static_cast<u16*>(p.O) + out_row(p, w, r, at_lse) + d;
+        *reinterpret_cast<uint2*>(dst) = uint2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+      } else {
+        *reinterpret_cast<f32x4*>(p.part_o + ((long long)seg.slot * kStreamRows + r) * D + d) = x;
       }
     }
   });
@@ -358,7 +363,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
   const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 
   for_segments<kTileThreads>(p, scan, [&](const Segment& seg) {
-    const PairView w = PairView::uniform(p, seg.pair);
+    const PairView w = seg.w;
     const bool active = seg.r0 + wave * 32 < w.M;        // wave-uniform: the others only copy
     const int rc = min(seg.r0 + wave * 32 + ln, w.M - 1);
     const int qvis = w.visible(p, rc / c.G) - 4 * h;     // compared with rows of a tile that leave out 4 h
@@ -389,7 +394,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
       if (threadIdx.x == 0) sMissing = 0;
       __syncthreads();
       for (int i = threadIdx.x; i < tab_end - tab0; i += kTileThreads) {
-        const int page = p.pg.table[(long long)seg.pair * p.pg.pages_cap + tab0 + i];
+        const int page = p.pg.table[(long long)w.pair * p.pg.pages_cap + tab0 + i];
         const bool there = (unsigned)page < (unsigned)p.pg.n_pages;
         sTab[i] = there ? page : -1;
         if (!there) sMissing = 1;

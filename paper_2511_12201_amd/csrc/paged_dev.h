@@ -42,13 +42,13 @@ struct AttnParams {
 // Query rows and cache rows of a pair: row r is token r / G, head r % G of the group; how many rows a query row sees.
 struct PairView {
   int pair, b, g, cnt, end, M;
-  __device__ __forceinline__ PairView(const AttnParams& p, int pair_) : pair(pair_) {
+  __device__ __forceinline__ PairView(const AttnParams& p, int pair_, int cnt_, int end_) : pair(pair_), cnt(cnt_), end(end_) {
     b = pair / p.c.Hkv;
     g = pair - b * p.c.Hkv;
-    cnt = clampi(p.new_cnt[b], 0, p.c.n_new);
-    end = clampi(p.row_end[pair], 0, rows_cap(p.pg));
     M = cnt * p.c.G;
   }
+  __device__ __forceinline__ PairView(const AttnParams& p, int pair_)
+      : PairView(p, pair_, clampi(p.new_cnt[pair_ / p.c.Hkv], 0, p.c.n_new), clampi(p.row_end[pair_], 0, rows_cap(p.pg))) {}
   // the view of a pair that the whole wavefront works on: addresses and bounds made of it stay in scalar registers
   __device__ static __forceinline__ PairView uniform(const AttnParams& p, int pair) {
     PairView w(p, pair);
@@ -106,19 +106,29 @@ __device__ __forceinline__ int span_of(int b, int n) {
 }
 
 struct Segment {
-  int item, pair, r0, u0, u1, slot;
+  PairView w;
+  int item, r0, u0, u1, slot;
   bool whole;
 };
 
 // Walks a workgroup's span: f(segment) for its part of every item in it.  All threads call it.  Up to 64 items (a few sequences of
-// few tokens, where the start counts) every wavefront finds its place by itself, one item a lane; more are added up by the workgroup.
+// few tokens, where the start counts) every wavefront finds its place by itself, one item a lane that keeps the item's lengths (loaded
+// anew for every use they cost 2 of the 7 us of a token on 4109 rows); more are added up by the workgroup.
 template <int THREADS, typename F>
 __device__ __forceinline__ void for_segments(const AttnParams& p, Scan& s, F f) {
   Spans sp;
   u64 begin, at_item;                                    // where the span begins, and its first item
   int item, w;
-  if (p.n_items <= 64) {
-    const int mine = lane_id() < p.n_items ? item_units(p, lane_id()) : 0;
+  int lane_cnt = 0, lane_end = 0;
+  if (__builtin_expect(p.n_items <= 64, true)) {
+    int mine = 0;
+    if (lane_id() < p.n_items) {
+      const int pair = lane_id() / p.tiles_per_pair;
+      const PairView v(p, pair);
+      mine = item_units(p, v, (lane_id() - pair * p.tiles_per_pair) * p.tm);
+      lane_cnt = v.cnt;
+      lane_end = v.end;
+    }
     const u64 inc = wave_scan((u64)mine);
     sp.cut(__shfl(inc, 63, 64), p.n_wgs, p.min_share);
     if (sp.total == 0 || (int)blockIdx.x >= sp.n) return;
@@ -162,16 +172,13 @@ __device__ __forceinline__ void for_segments(const AttnParams& p, Scan& s, F f) 
   item = __builtin_amdgcn_readfirstlane(item);
   int off = __builtin_amdgcn_readfirstlane((int)(begin - at_item));
   for (u64 pos = begin; pos < end; ++item) {
-    const int units = __builtin_amdgcn_readfirstlane(item_units(p, item));
+    const int pair = item / p.tiles_per_pair, r0 = (item - pair * p.tiles_per_pair) * p.tm;
+    const PairView view = p.n_items <= 64 ? PairView(p, pair, __builtin_amdgcn_readlane(lane_cnt, item & 63), __builtin_amdgcn_readlane(lane_end, item & 63))
+                                          : PairView::uniform(p, pair);
+    const int units = __builtin_amdgcn_readfirstlane(item_units(p, view, r0));
     if (units == 0) continue;
     const int take = (int)min((u64)(units - off), end - pos), tiles = units - p.over;
-    Segment seg;
-    seg.item = item;
-    seg.pair = item / p.tiles_per_pair;
-    seg.r0 = (item - seg.pair * p.tiles_per_pair) * p.tm;
-    seg.u0 = max(off - p.over, 0);
-    seg.u1 = off + take - p.over;
-    seg.slot = 2 * w + (pos == begin ? 0 : 1);
+    Segment seg{view, item, r0, max(off - p.over, 0), off + take - p.over, 2 * w + (pos == begin ? 0 : 1), false};
     seg.whole = seg.u0 == 0 && seg.u1 == tiles;
     if (seg.u1 > seg.u0) {
       if (seg.u0 == 0 && threadIdx.x == 0)               // who joins the item finds its slots here (whole: first span = last)

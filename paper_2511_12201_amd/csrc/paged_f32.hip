@@ -30,7 +30,7 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 1 : 2) void paged_attn_f32_kernel
   const float c2 = c.scale * kLog2e;
 
   for_segments<kThreads>(p, scan, [&](const Segment& seg) {
-    const PairView w = PairView::uniform(p, seg.pair);
+    const PairView w = seg.w;
     const int r = seg.r0 + (SPLIT ? 0 : wave * 32) + ln;
     const bool real = r < w.M;
     const int rc = min(r, w.M - 1);
