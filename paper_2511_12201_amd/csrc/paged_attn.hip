@@ -407,15 +407,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
       const int n_plain = missing ? 0 : min(nt, w.end / kTileKeys - c0);              // whole tiles come first
       const int n_full = missing ? 0 : min(seen_by_all / kTileKeys - c0, nt);         // tiles in which nothing is masked
 
-      auto issue_part = [&](int t, int part) {           // one load instruction of tile c0 + t: part < LPH is K
-        const unsigned dst = lds_base + (unsigned)(t % kStages) * kStageBytes;
-        const bool is_k = part < LPH;
-        const int at = (is_k ? part : part - LPH) * kTileWaves + wave;
-        const int j = (c0 + t) * kTileKeys + at * RPI;
-        const int page = __builtin_amdgcn_readfirstlane(sTab[(j >> p.pg.shift) - tab0]);
-        const long long row = ((long long)page << p.pg.shift) + (j & ((1 << p.pg.shift) - 1));
-        if (is_k) gload_lds16(Kpool + row * RB, src_k, dst + at * 1024);
-        else gload_lds16(Vpool + row * RB, src_v, dst + kKBytes + at * 1024);
+      // a wavefront's share of a tile: LPH times RPI rows, K and V alike; `entry` is their page
+      auto first_row = [&](int t, int part) { return (c0 + t) * kTileKeys + (part * kTileWaves + wave) * RPI; };
+      auto entry = [&](int t, int part) { return sTab[(first_row(t, part) >> p.pg.shift) - tab0]; };
+      auto bytes_at = [&](int t, int part, int page) {
+        page = __builtin_amdgcn_readfirstlane(page);
+        return (((long long)page << p.pg.shift) + (first_row(t, part) & ((1 << p.pg.shift) - 1))) * RB;
+      };
+      auto copy_part = [&](int t, int part, bool is_k, long long from) {     // one load instruction
+        const unsigned dst = lds_base + (unsigned)(t % kStages) * kStageBytes + (part * kTileWaves + wave) * 1024;
+        if (is_k) gload_lds16(Kpool + from, src_k, dst);
+        else gload_lds16(Vpool + from, src_v, dst + kKBytes);
       };
       auto row_there = [&](int j) { return j < w.end ? sTab[(j >> p.pg.shift) - tab0] : -1; };
       auto copy_tile = [&](int t) {                      // a tile that is not whole; every load before ends here, as the counts of the waits assume
@@ -437,7 +439,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
       auto issue_tile = [&](int t) {
         if (t < n_plain) {
 #pragma unroll
-          for (int j = 0; j < LPT; ++j) issue_part(t, j);
+          for (int part = 0; part < LPH; ++part) {
+            const long long from = bytes_at(t, part, entry(t, part));
+            copy_part(t, part, true, from);
+            copy_part(t, part, false, from);
+          }
         } else {
           copy_tile(t);
         }
@@ -499,6 +505,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
         return pack_bf16x2(a, b);
       };
       union PFrag { bf16x8 v[4]; unsigned u[16]; };
+      // The pages of this wavefront's shares of kGroup tiles, a lane each: a look-up in every step would wait for the fragments on their
+      // way (2048 tokens on 65536 rows: 1685 us; looked up a step ahead 1653; so 1628).
+      constexpr int kGroup = 64 / LPH;
+      int pages = 0;
+      auto load_pages = [&](int t) { pages = entry(min(t + lane / LPH, n_plain - 1), lane % LPH); };
+      if (n_plain > 0) load_pages(0);
 
       // One step: weights of tile t from sc and O += V(t) P(t); where there is a tile t + 1, its scores into sn under the
       // weights, and their maximum under the second product.  kSteady: there is one, and tile t + 3 is whole and issued here.
@@ -510,6 +522,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
         const unsigned stage = (unsigned)(t % kStages) * kStageBytes, stage_n = (unsigned)((t + 1) % kStages) * kStageBytes;
         PFrag pf;
         float lsum = 0.f;
+        long long from[LPH];                             // where the share of tile t + 3 begins
         bf16x8 vf[kAhead];
         constexpr int EQ = 32 / NQK;
         if (has_next) {
@@ -518,6 +531,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
           __syncthreads();                               // and everyone's; tile t - 1 is done with
           if (!kSteady && t + 3 < nt) issue_tile(t + 3);
           __builtin_amdgcn_sched_barrier(0);
+          if (kSteady && (t + 3) % kGroup == 0) load_pages(t + 3);
+#pragma unroll
+          for (int part = 0; kSteady && part < LPH; ++part) from[part] = bytes_at(t + 3, part, __builtin_amdgcn_readlane(pages, (t + 3) % kGroup * LPH + part));
           bf16x8 kf[kAhead];
 #pragma unroll
           for (int i = 0; i < kAhead; ++i) kf[i] = kfrag(stage_n, i);
@@ -529,7 +545,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
             else vf[i + kAhead - NQK] = vfrag(stage, i + kAhead - NQK);
 #pragma unroll
             for (int e = 0; e < EQ; e += 2) pf.u[(i * EQ + e) / 2] = weights(sc, i * EQ + e, lsum);
-            if (kSteady && i * LPH % NQK == 0) issue_part(t + 3, i * LPH / NQK);
+            if (kSteady && i * LPH % NQK == 0) copy_part(t + 3, i * LPH / NQK, true, from[i * LPH / NQK]);
           }
         } else {
 #pragma unroll
@@ -559,7 +575,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
               mloc = fmaxf(fmaxf(sn[x / 16][x % 16], sn[x / 16][x % 16 + 1]), mloc);
             }
           }
-          if (kSteady && i * LPH % NPV == 0) issue_part(t + 3, LPH + i * LPH / NPV);
+          if (kSteady && i * LPH % NPV == 0) copy_part(t + 3, i * LPH / NPV, false, from[i * LPH / NPV]);
         }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
