@@ -191,6 +191,19 @@ __device__ __forceinline__ void gload_lds16(const void* sbase, unsigned lane_off
       : "v"(lane_off), "s"(sbase), "s"(lds_addr)
       : "memory");
 }
+// The same for data that nobody reads again soon: it does not push out what the caches hold.
+__device__ __forceinline__ void gload_lds16_once(const void* sbase, unsigned lane_off, unsigned lds_addr) {
+  unsigned saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %3\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2 nt\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(lane_off), "s"(sbase), "s"(lds_addr)
+      : "memory");
+}
 // 4 bytes per lane, global -> LDS at lds_addr + lane * 4
 __device__ __forceinline__ void gload_lds4(const void* gptr, unsigned lds_addr) {
   unsigned saved;

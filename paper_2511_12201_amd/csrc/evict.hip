@@ -141,7 +141,9 @@ __device__ __forceinline__ void move_rows(const EvictParams& p, const PairRows& 
     const int from = pool_row(p.pg, pair, m.x), to = pool_row(p.pg, pair, m.y);
     if (from < 0 || to < 0) continue;
     for (int c = lane; c < per; c += LANES) {
-      const u32x4 k = static_cast<const u32x4*>(p.pg.K)[(long long)from * per + c], v = static_cast<const u32x4*>(p.pg.V)[(long long)from * per + c];
+      // nobody reads them there again (131072 rows to 32768: 76.4 / 72.6 us)
+      const u32x4 k = __builtin_nontemporal_load(static_cast<const u32x4*>(p.pg.K) + (long long)from * per + c);
+      const u32x4 v = __builtin_nontemporal_load(static_cast<const u32x4*>(p.pg.V) + (long long)from * per + c);
       static_cast<u32x4*>(p.pg.K)[(long long)to * per + c] = k;
       static_cast<u32x4*>(p.pg.V)[(long long)to * per + c] = v;
     }

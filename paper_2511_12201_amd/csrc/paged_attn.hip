@@ -27,9 +27,9 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // A wavefront takes 32 cache rows per trip, K and V straight from the pages into a ring of two LDS stages of its own: while one is
 // worked on the other is on its way, 64 to 128 KB per CU in flight, and no barrier in the loop.  (Loads through registers, three
 // workgroups a CU, kept less in flight: 131k rows of eight sequences and four KV heads of 128 elements, a token each, took 567 us
-// with the weights, 468 now; 378 without them, 5.7 TB/s where a copy, which also writes, reaches 5.1.)  An instruction takes 1024
-// bytes, whole rows of one page; the pieces of a row change places as in the tile kernel below.  Blocks that are not whole go through
-// registers.
+// with the weights, 415 now; 338 without them, 6.35 TB/s where a copy, which also writes, reaches 5.1.)  An instruction takes 1024
+// bytes, whole rows of one page; the pieces of a row change places as in the tile kernel below.  Blocks with pages that are not there
+// go through registers.
 constexpr int kStreamWaves = 4, kStreamThreads = kStreamWaves * 64, kStreamRows = 32;
 
 // where the 16-byte pieces of row r of a tile lie: piece c at c ^ swz(r)
@@ -87,6 +87,9 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
     auto half_row = [&](int block, int half, int page) {
       return (unsigned)page < (unsigned)p.pg.n_pages ? (page << p.pg.shift) + ((block * 32 + half * 16) & page_mask) : -1;
     };
+    // Rows pass by once, so they are loaded as such (one token of eight sequences on 131089 rows 378 / 338 us, 6.35 TB/s; with scores 506
+    // / 453), unless scores are kept and the infinity cache holds most rows from call to call (131089 rows, 268 MB: 64 / 69).
+    const bool once = !LOGITS || seg.total * (kStreamWaves * 32) * (2 * RB) > 320ull << 20;
     // K or V of a block into a stage
     auto issue = [&](auto is_k, int block, int stage, int row_a, int row_b) {
       constexpr bool kIsK = decltype(is_k)::value;
@@ -97,7 +100,8 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
 #pragma unroll
         for (int i = 0; i < LPH; ++i) {
           const long long row = (long long)(i * RPI < 16 ? row_a : row_b) + i * RPI % 16;
-          gload_lds16(pool + row * RB, kIsK ? src_k[i % NP] : src_v, own_ring + at + i * 1024);
+          if (once) gload_lds16_once(pool + row * RB, kIsK ? src_k[i % NP] : src_v, own_ring + at + i * 1024);
+          else gload_lds16(pool + row * RB, kIsK ? src_k[i % NP] : src_v, own_ring + at + i * 1024);
         }
       } else if (row_a >= 0 && (row_b >= 0 || last_row < 16)) {          // the last rows: behind the last one it again, which is masked
 #pragma unroll

@@ -109,6 +109,7 @@ struct Segment {
   PairView w;
   int item, r0, u0, u1, slot;
   bool whole;
+  u64 total;                                             // units of all items
 };
 
 // Walks a workgroup's span: f(segment) for its part of every item in it.  All threads call it.  Up to 64 items (a few sequences of
@@ -199,7 +200,7 @@ __device__ __forceinline__ void for_segments(const AttnParams& p, Scan& s, F f) 
     }
     if (units == 0) continue;
     const int from = at < begin ? (int)(begin - at) : 0, to = (int)min((u64)units, end - at);
-    Segment seg{view, it, r0, max(from - p.over, 0), to - p.over, 2 * w + (at <= begin ? 0 : 1), false};
+    Segment seg{view, it, r0, max(from - p.over, 0), to - p.over, 2 * w + (at <= begin ? 0 : 1), false, sp.total};
     seg.whole = seg.u0 == 0 && to == units;
     if (seg.u1 > seg.u0) {
       if (seg.u0 == 0 && threadIdx.x == 0)               // who joins the item finds its slots here (whole: first span = last)

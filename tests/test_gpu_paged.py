@@ -247,6 +247,7 @@ LONG = [
     ((14, 2), 128, 1, 64, (9000, 4097), True), ((8, 2), 64, 3, 16, (20011, 64), True), ((4, 1), 128, 16, 32, (3000, 2999), False),
     ((14, 2), 128, 100, 64, (4000, 1531), True), ((6, 2), 64, 333, 16, (2222, 900), True), ((4, 1), 128, 24, 16, (70001, 33000), True),
     ((2, 1), 64, 700, 256, (700, 699), True), ((8, 1), 128, 64, 16, (6400, 6401), False), ((32, 1), 64, 9, 32, (5003, 17), True),
+    ((8, 4), 128, 2, 64, (99990, 90001), True),              # more than the caches hold: 389 MB in bf16
 ]
 
 
@@ -436,6 +437,31 @@ def test_append(dtype, D, rot, n, turned):
         want = po.rope(host(Q)[b, :, :new_cnt[b]], pos[b] + np.arange(new_cnt[b]), freq, True)
         within(host(Qout)[b, :, :new_cnt[b]], want, rope_bar(host(Q)[b, :, :new_cnt[b]], want, rot, True, dtype), "Q")
         assert (Qout[b, :, new_cnt[b]:] == 3.0).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_rows_are_turned_as_few(D):
+    """Calls beyond what the caches hold (128 MB in and out) against the same rows in parts, bit for bit."""
+    rng = np.random.default_rng(D)
+    n, H, Hkv = 16384 * 64 // D + 37, 28, 4
+    Q, K, V = (rand(rng, 1, h, n, D, dtype=BF16) for h in (H, Hkv, Hkv))
+    plan = ob.make_rope_desc(D, base=1e6)
+    for backward in (False, True):
+        q, k = ob.omni_rope(plan, layer(Q, K), Q, K, backward=backward)
+        for a in range(0, n, 1500):
+            pq, pk = Q[:, :, a:a + 1500].contiguous(), K[:, :, a:a + 1500].contiguous()
+            pos = torch.arange(a, a + pq.shape[2], dtype=torch.int32, device="cuda")[None]
+            wq, wk = ob.omni_rope(plan, layer(pq, pk), pq, pk, pos, backward=backward)
+            assert torch.equal(q[:, :, a:a + 1500], wq) and torch.equal(k[:, :, a:a + 1500], wk)
+    one, parts = (Cache(np.random.default_rng(1), 1, Hkv, n // 64 + 1, 64, D, BF16) for _ in range(2))
+    row_pos = torch.zeros(1, Hkv, one.cap, dtype=torch.int32, device="cuda")
+    q, _ = ob.omni_paged_append(ob.make_chunk_desc(Q, K), plan, Q, K, V, one.pool, ints([7]), ints([n]), ints([[0] * Hkv]), row_pos)
+    for a in range(0, n, 1500):
+        pq, pk, pv = (x[:, :, a:a + 1500].contiguous() for x in (Q, K, V))
+        wq, _ = ob.omni_paged_append(ob.make_chunk_desc(pq, pk), plan, pq, pk, pv, parts.pool, ints([7 + a]), ints([pq.shape[2]]),
+                                     ints([[a] * Hkv]), row_pos)
+        assert torch.equal(q[:, :, a:a + 1500], wq)
+    assert torch.equal(one.K, parts.K) and torch.equal(one.V, parts.V)
 
 
 def test_append_of_counts_out_of_range():
