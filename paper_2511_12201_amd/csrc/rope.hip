@@ -87,9 +87,10 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p) {
   if constexpr (APPEND) position = (int)((unsigned)p.pos[b] + (unsigned)n);
   else if (p.pos) position = p.pos[(long long)b * p.N + n];
 
-  // where the chunk's two runs of eight lie: the members of eight pairs, or 16 neighbours (pairs side by side; what is not turned)
+  // where the chunk's two runs of eight lie, in the two halves of what is turned or of what is not: neighbouring threads have
+  // neighbouring runs.  Turned, they are the members of eight pairs, or (pairs side by side) two times four pairs.
   const bool turned = c < p.rot / 16;
-  const int at0 = !INTER && turned ? 8 * c : 16 * c, at1 = !INTER && turned ? p.rot / 2 + 8 * c : 16 * c + 8;
+  const int at0 = turned ? 8 * c : p.rot + 8 * (c - p.rot / 16), at1 = at0 + (turned ? p.rot : D - p.rot) / 2;
   float cs[8], sn[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeParams p) {
   if (turned) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const double turns = (double)position * p.f[8 * c + e];
+      const double turns = (double)position * p.f[INTER ? 4 * c + (e < 4 ? e : p.rot / 4 + e - 4) : 8 * c + e];
       float s, co;
       sincospif(2.f * (float)(turns - rint(turns)), &s, &co);
       cs[e] = co * p.out_scale;
@@ -174,15 +175,15 @@ int launch(RopeParams& p, int dtype, int D, bool inter, hipStream_t st) {
   p.heads_per_block = (int)std::max(1ll, std::min((long long)n_heads, (long long)n_heads * blocks * p.B / 1024));
   const dim3 grid(blocks, cdiv(n_heads, p.heads_per_block), p.B);
   // Beyond what the L2s hold (32 MB, in and out) the rows pass by once: 65536 tokens of 32 heads 205 / 194 us, 13312 tokens to the
-  // pages 56 / 52.  Not where a line takes two instructions (pairs side by side, parts of a head that are not turned, fp32): 111 / 120.
-  const bool once = dtype == OMNI_BF16 && !inter && p.rot == D && (long long)p.B * p.N * n_heads * D * 4 > 64ll << 20;
+  // pages 56 / 52.  Not where a line of 128 bytes takes two instructions (fp32, short heads, heads turned in part: 108 / 123).
+  const bool once = dtype == OMNI_BF16 && D == 128 && p.rot == D && (long long)p.B * p.N * n_heads * D * 4 > 64ll << 20;
 #define OMNI_ROPE(T, DD, I, O)                                  \
   if (D == DD && inter == I && once == O) rope_kernel<T, DD, I, APPEND, O><<<grid, kThreads, 0, st>>>(p)
 #define OMNI_ROPE_T(T)                                          \
   OMNI_ROPE(T, 64, false, false); else OMNI_ROPE(T, 64, true, false); else OMNI_ROPE(T, 128, false, false); else OMNI_ROPE(T, 128, true, false)
   if (dtype == OMNI_BF16) {
-    OMNI_ROPE(u16, 64, false, true);
-    else OMNI_ROPE(u16, 128, false, true);
+    OMNI_ROPE(u16, 128, false, true);
+    else OMNI_ROPE(u16, 128, true, true);
     else OMNI_ROPE_T(u16);
   } else {
     OMNI_ROPE_T(float);

@@ -439,13 +439,13 @@ def test_append(dtype, D, rot, n, turned):
         assert (Qout[b, :, new_cnt[b]:] == 3.0).all()
 
 
-@pytest.mark.parametrize("D", [64, 128])
-def test_many_rows_are_turned_as_few(D):
+@pytest.mark.parametrize("D,rot,interleaved", [(128, 128, False), (128, 128, True), (128, 48, False), (64, 64, True)])
+def test_many_rows_are_turned_as_few(D, rot, interleaved):
     """Calls beyond what the caches hold (128 MB in and out) against the same rows in parts, bit for bit."""
     rng = np.random.default_rng(D)
     n, H, Hkv = 16384 * 64 // D + 37, 28, 4
     Q, K, V = (rand(rng, 1, h, n, D, dtype=BF16) for h in (H, Hkv, Hkv))
-    plan = ob.make_rope_desc(D, base=1e6)
+    plan = ob.make_rope_desc(D, rot, base=1e6, interleaved=interleaved)
     for backward in (False, True):
         q, k = ob.omni_rope(plan, layer(Q, K), Q, K, backward=backward)
         for a in range(0, n, 1500):
