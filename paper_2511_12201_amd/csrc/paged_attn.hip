@@ -777,9 +777,9 @@ struct Plan {
   bool logits;                                           // scores of the pass are kept for the weights
 };
 
-// Pairs of at most 32 query rows stream the cache.  us a call, stream / tiles, 28 heads on 4: one token on 131089 rows 55 / 85, four
-// tokens on 4109 rows 14 / 22, on 131089 of eight sequences 391 / 405, with weights 654 / 721; 32 heads on 4 of 64 elements, four
-// tokens on 4109 rows 13.8 / 15.5, on 131089 of eight sequences 204 / 189.  Above, a stream would read the cache twice.
+// Pairs of at most 32 query rows stream the cache.  us a call, stream / tiles, 28 heads on 4: one token on 131089 rows 53 / 88, four
+// tokens on 4109 rows 14 / 23, on 131089 of eight sequences 341 / 405, with weights 587 / 723; 32 heads on 4 of 64 elements, four
+// tokens on 4109 rows 13 / 17, on 131089 of eight sequences 177 / 191.  Above, a stream would read the cache twice.
 // Workgroups: what the chip holds at once (LDS: one a CU, two of the streams and of the fp32 tiles with their small stages).
 Plan make_plan(const Chunk& c, int dtype, int weight_rows) {
   const bool few = c.G * c.n_new <= kStreamRows, bf16 = dtype == OMNI_BF16;

@@ -211,7 +211,7 @@ __global__ __launch_bounds__(kThreads) void paged_weights_f32_kernel(AttnParams 
 // rows go from memory straight into a ring of four LDS stages, three on their way while one is worked on, one barrier a tile.  The
 // scores of 32 query rows are formed under the weights of the 32 before: per 64 x 32 weights a wavefront issues 16 matrix
 // instructions (512 cycles) and 32 times scale, 2^x and sum (950 cycles with the four that each 2^x takes): the vector ALU bounds it.
-// 500 new tokens in four sequences of 8200 to 16400 rows: 190 us, 114 if nothing but those instructions counted; the rest is what a
+// 500 new tokens in four sequences of 8200 to 16400 rows: 196 us, 114 if nothing but those instructions counted; the rest is what a
 // block of cache rows costs to take up (11 us of the 65 us that its tiles take) and the second workgroup of a CU, which works alone
 // once the first, older one is through.
 constexpr int kBfKeys = 64, kBfRows = kWaves * kBfKeys, kBfQ = 64, kBfStages = 4;
