@@ -193,7 +193,7 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
       }
       if constexpr (LOGITS) {
         // through LDS, so that a store writes whole lines: rows of 32 scores, 8 of them per instruction (16 bytes a lane straight from
-        // the accumulators, a quarter of a line per instruction: no faster with 117 MB of them beside 2.1 GB of rows, but the pass that adds them up reads them at 4.6 TB/s)
+        // the accumulators, a quarter of a line per instruction: no faster here, but the pass that adds them up reads whole lines)
         unsigned char* out = sQ + wave * kScoreBytes;
         float* dst = p.logits + ((long long)w.pair * cdiv(rows_cap(p.pg), 32) + block) * (c.G * c.n_new) * 32;
 #pragma unroll
@@ -323,13 +323,14 @@ int launch_stream(const AttnParams& p, hipStream_t st) {
 // ------------------------------------------------------------------ many query rows: tiles in LDS
 
 // 512 threads = 8 wavefronts x 32 query rows.  K and V tiles of 64 rows go from the pages straight into LDS (global_load_lds), row by
-// row: an instruction takes 4 (D = 128) or 8 (D = 64) whole rows, which lie in one page (page_rows >= 16), so that a page costs
-// one wave-uniform table entry.  A row's 16-byte pieces change places inside the row as they are written (the lanes' addresses do
-// it): K piece c of row r goes to c ^ (r % 16) (D = 64: c ^ (r / 2 % 8)), so that the 16 lanes that read one piece of 16 rows meet every bank once; V
-// piece c to c ^ 4 (r % 4) (D = 64: c ^ 4 (r / 2 % 2)), so that the transposing reads of 4 rows do.  Ring of four stages, so up to three tiles are in flight
-// while one is computed and one barrier per tile is enough; the waits are counted by hand (the compiler would wait for every
-// load in flight).  Tiles that are not whole (the last one, missing pages) are copied through registers with zeros for what is
-// not there.
+// row: an instruction takes 4 (D = 128) or 8 (D = 64) whole rows, which lie in one page (page_rows >= 16), so that a page costs one
+// wave-uniform table entry.  A row's 16-byte pieces change places inside the row as they are written (the lanes' addresses do it): K
+// piece c of row r goes to c ^ (r % 16) (D = 64: c ^ (r / 2 % 8)), so that the 16 lanes that read one piece of 16 rows meet every
+// bank once; V piece c to c ^ 4 (r % 4) (D = 64: c ^ 4 (r / 2 % 2)), so that the transposing reads of 4 rows do.  Ring of four
+// stages, so up to three tiles are in flight while one is computed and one barrier per tile is enough; the waits are counted by hand
+// (the compiler would wait for every load in flight).  2048 tokens of 28 heads on 65536 rows: 1.59 ms, 1.20 PFLOP/s of the 1.34 that
+// a large product reaches; the power limit bounds it (25 calls in a row: 1.68).  Tiles that are not whole (the last one, missing
+// pages) are copied through registers with zeros for what is not there.
 constexpr int kTileWaves = 8, kTileThreads = kTileWaves * 64, kTileRows = kTileWaves * 32;
 constexpr int kTileKeys = 64, kStages = 4;
 constexpr int kTab = 2048;                               // page table entries in LDS: 512 tiles of the smallest pages

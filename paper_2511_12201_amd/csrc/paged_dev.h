@@ -4,10 +4,10 @@
 // sees, in units of `unit` rows, and counts `over` units more for what it costs to take it up (2048 tokens on as many rows: the
 // workgroup with the first, short items of a pair had six of them and took 97 us where the others took 50).  All units of all items,
 // item after item, are one line that is cut into as many equal spans as there are workgroups: every workgroup does the same amount of
-// work whatever the lengths are, and the lengths stay on the device.  A workgroup that has all units of an item writes its output rows; otherwise it leaves a partial state (maximum, sum,
-// weighted rows) in one of its two slots (its span's first item: slot 2 w, another one: it can only be the last: 2 w + 1), and
-// the paged_combine kernels join the slots of an item in the order of the units: equal inputs, equal bits.  The workgroup that has an
-// item's first unit writes down which spans share it.
+// work whatever the lengths are, and the lengths stay on the device.  A workgroup that has all units of an item writes its output
+// rows; otherwise it leaves a partial state (maximum, sum, weighted rows) in one of its two slots (its span's first item: slot 2 w,
+// another one: it can only be the last: 2 w + 1), and the paged_combine kernels join the slots of an item in the order of the units:
+// equal inputs, equal bits.  The workgroup that has an item's first unit writes down which spans share it.
 #pragma once
 
 #include "paged.h"

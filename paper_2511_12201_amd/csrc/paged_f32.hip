@@ -4,7 +4,8 @@
 // product's sum, so that a lane reads its half of a K row 16 bytes at a time, and the accumulators of S^T are the second product's
 // B operand as they stand (register i holds row 8 (i / 4) + 4 h + i % 4).  Two divisions of labour: four wavefronts of 32 query rows
 // that share 32-row tiles of the cache, or, for pairs of at most 32 query rows, four wavefronts that take 32-row tiles of their own
-// and join their states.  The matrix instructions bound it (64 cycles each, D of them per 32 x 32 tile).
+// and join their states.  The matrix instructions bound it (64 cycles each, D of them per 32 x 32 tile): 256 tokens of 28 heads on 8192
+// rows of 128 elements 265 us, 113 TFLOP/s of the 154 that a large product reaches.
 #include "paged_dev.h"
 
 namespace omni {
