@@ -912,13 +912,14 @@ _DTYPES = {OMNI_BF16: torch.bfloat16, OMNI_F32: torch.float32}
 
 # the stream that torch works on, as a number: the public accessor builds an object first (2.5 us of a call's 14)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _run_on(dev: torch.device, fn, *args):
     """fn(*args, stream) on the tensors' device and its current stream."""
     if dev.type != "cuda":
         raise ValueError(f"tensors must be on the GPU, not on {dev}")
-    if dev.index == torch.cuda.current_device():
+    if dev.index == _current_device():
         rc = fn(*args, _raw_stream(dev.index))
     else:
         with torch.cuda.device(dev):
@@ -973,7 +974,7 @@ def _pool_of(pool: PagePool, dtype, head_dim: int, dev):
 
 
 def _pairs_desc(pool: PagePool) -> ChunkDesc:
-    """The pairs of a pool's table as omni_paged_evict describes them; made once per pool."""
+    """The pairs of a pool's table as omni_paged_evict describes them, and the scratch it takes; made once per pool."""
     d = getattr(pool, "_pairs", None)
     if d is None:
         K, _, table = pool._keep
@@ -981,6 +982,7 @@ def _pairs_desc(pool: PagePool) -> ChunkDesc:
         d.batch, d.n_kv_heads, d.head_dim, d.dtype = *table.shape[:2], K.shape[2], _dtype_code(K)
         d.n_q_heads, d.n_new, d.causal, d.softmax_scale = d.n_kv_heads, 1, 1, 1.0
         d.q_stride = d.kv_stride = (C.c_int64 * 3)(d.n_kv_heads * d.head_dim, d.head_dim, d.head_dim)
+        d._scratch = workspace_bytes(CALL_PAGED_EVICT, d, pool.pages_cap * pool.page_rows)
     return d
 
 
@@ -1102,7 +1104,7 @@ def omni_paged_evict(pool: PagePool, budget: int, n_sink: int, n_recent: int, se
     else:
         _want("acc_out", acc_out, torch.float32, (B, Hkv, cap), dev)
     d = _pairs_desc(pool)
-    buf = _scratch(ws, CALL_PAGED_EVICT, d, cap, dev)
+    buf = torch.empty(d._scratch, dtype=torch.uint8, device=dev) if ws is None else ws.get(CALL_PAGED_EVICT, d, cap)
     _run_on(dev, load_library().omni_paged_evict, C.byref(d), C.byref(pool), budget, n_sink, n_recent, seq_len.data_ptr(),
             row_end.data_ptr(), row_pos.data_ptr(), acc.data_ptr(), row_cnt.data_ptr(), row_pos_out.data_ptr(),
             acc_out.data_ptr(), buf.data_ptr(), buf.numel())
