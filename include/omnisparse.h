@@ -795,6 +795,13 @@ int omni_debug_device_work_list(const omni_layer_desc* desc, const int32_t* q_id
                                 int64_t* layout, void* stream);
 
 /*
+ * Diagnostic: host mirror of the selection that omni_paged_evict makes where rows_cap <= 16384: the
+ * same steps on the 32-bit keys that rows are ranked by.  keys, stay [n] are HOST pointers; stay[j] = 1 for
+ * the `keep` rows of largest key, equal ones by lowest row; 1 <= keep < n.
+ */
+int omni_debug_evict_stay(const uint32_t* keys, int32_t n, int32_t keep, uint8_t* stay);
+
+/*
  * Diagnostic: copy `bytes` (a positive multiple of 16) from src to dst, both DEVICE pointers
  * to 16-byte aligned, non-overlapping buffers, with a plain copy kernel
  * (calibration_copy_kernel) on `stream`.  A launch of known HBM traffic: a profiler's

@@ -37,6 +37,7 @@ EXPORTED = [
     "omni_slim_decode_grouped_static", "omni_static_scratch_bytes",
     "omni_sparse_prefill", "omni_sparse_prefill_workspace_bytes", "omni_slim_decode_prepare",
     "omni_rope_frequencies", "omni_rope", "omni_paged_append", "omni_paged_attn", "omni_paged_evict",
+    "omni_debug_evict_stay",
 ]
 
 PROF_KERNELS = {"attn_fwd": 0, "pack_kv": 1, "clear_out": 2, "pool_q": 3, "probe_lse": 4, "probe_sum": 5,
@@ -164,6 +165,7 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.omni_paged_attn.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.omni_paged_evict.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.omni_profile_enable.argtypes = [C.c_int]
+    lib.omni_debug_evict_stay.argtypes = [vp, i32, i32, vp]
     lib.omni_debug_copy.argtypes = [vp, vp, sz, vp]
     lib.omni_debug_key_split_len.argtypes = [C.c_int]
     lib.omni_debug_attention_route.argtypes = [C.c_int]
@@ -319,6 +321,15 @@ def debug_device_work_list(desc: LayerDesc, q_idx, q_cnt, kv_idx, budget, tile_r
     h = buf.cpu().numpy()
     n = int(h[1])
     return h[layout[1]: layout[1] + 2 * n].reshape(n, 2), h[layout[2]: layout[2] + n], h[4:12], h[12:20]
+
+
+def debug_evict_stay(keys, keep: int):
+    """Host mirror of eviction's selection: which of the rows with these keys (uint32 array) stay, as a bool array."""
+    import numpy as np
+    keys = np.ascontiguousarray(keys, dtype=np.uint32)
+    stay = np.zeros(len(keys), dtype=np.uint8)
+    _check(load_library().omni_debug_evict_stay(keys.ctypes.data, len(keys), keep, stay.ctypes.data))
+    return stay.astype(bool)
 
 
 def debug_copy(src, dst):

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "common.h"
+#include "evict_cut.h"
 #include "kernels.h"
 #include "paged.h"
 #include "sched.h"
@@ -389,6 +390,40 @@ int omni_debug_copy(const void* src, void* dst, size_t bytes, void* stream) {
   REQUIRE_PTR(src); REQUIRE_PTR(dst);
   if (bytes == 0 || bytes % 16) OMNI_FAIL(OMNI_ERR_INVALID, "bytes must be a positive multiple of 16");
   return run_calibration_copy(src, dst, bytes, static_cast<hipStream_t>(stream));
+}
+
+int omni_debug_evict_stay(const uint32_t* keys, int32_t n, int32_t keep, uint8_t* stay) {
+  clear_error();
+  REQUIRE_PTR(keys); REQUIRE_PTR(stay);
+  if (keep < 1 || keep >= n) OMNI_FAIL(OMNI_ERR_INVALID, "need 1 <= keep < n");
+  const KeyCut cut = find_cut(
+      keep,
+      [&](int, const KeyRange& r, int need) {
+        std::vector<int> bins(2048);
+        for (int j = 0; j < n; ++j)
+          if (r.holds(keys[j])) ++bins[r.bin_of(keys[j])];
+        int bin = 2047, above = 0;
+        while (bin > 0 && above + bins[bin] < need) above += bins[bin--];
+        return Found{bin, need - above, bins[bin]};
+      },
+      [&](int, const KeyRange& r, unsigned& smallest, unsigned& largest) {
+        smallest = ~0u;
+        largest = 0;
+        for (int j = 0; j < n; ++j)
+          if (r.holds(keys[j])) {
+            smallest = std::min(smallest, keys[j]);
+            largest = std::max(largest, keys[j]);
+          }
+      });
+  std::vector<int> in;                             // rows of the range: the larger keys stay, equal ones by lowest row
+  for (int j = 0; j < n; ++j) {
+    stay[j] = keys[j] >= cut.range.base && !cut.range.holds(keys[j]);
+    if (cut.range.holds(keys[j])) in.push_back(j);
+  }
+  if ((int)in.size() != cut.count) OMNI_FAIL(OMNI_ERR_INVALID, "the range at the cut holds %d keys, counted were %d", (int)in.size(), cut.count);
+  std::stable_sort(in.begin(), in.end(), [&](int a, int b) { return keys[a] > keys[b]; });
+  for (int i = 0; i < cut.need; ++i) stay[in[i]] = 1;
+  return OMNI_OK;
 }
 
 int omni_debug_key_split_len(int tiles) {

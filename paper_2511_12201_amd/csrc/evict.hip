@@ -15,6 +15,7 @@
 //    131072 rows leave, 8 pairs: 5.2 + 6.4 + 6.1 + 10.2 + 39 us, the last at the rate of a copy.
 #include <algorithm>
 
+#include "evict_cut.h"
 #include "paged.h"
 
 namespace omni {
@@ -23,7 +24,6 @@ namespace {
 
 constexpr int kSmallRows = 16384, kSmallThreads = 1024;
 constexpr int kFewMoves = 256;                 // moves that the workgroup of a pair makes itself
-constexpr int kRanked = 128;                   // keys of a bin that are compared with one another instead of counted by digits
 constexpr int kBins = 2048;
 constexpr int kChunks = 40, kChunkThreads = 512, kChunkRows = 8;     // 38 whole chunks of at most 4096 rows: 155k rows in one round
 
@@ -97,10 +97,6 @@ __device__ __forceinline__ unsigned wave_umax(unsigned v) {
   return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
 }
 
-// The bin that holds the need-th largest key, how many of it are wanted, and how many it holds.
-struct Found {
-  int bin, left, count;
-};
 // From a histogram in LDS; all threads of evict_small_kernel call it.
 __device__ __forceinline__ Found find_bin(const int* hist, int need, int* wave_sums, int* out) {
   constexpr int PER = kBins / kSmallThreads, kWaves = kSmallThreads / 64;
@@ -231,82 +227,68 @@ __global__ __launch_bounds__(kSmallThreads) void evict_small_kernel(EvictParams 
   if (w.keep < w.n) {
 #pragma unroll
     for (int k = 0; k < R; ++k) key[k] = w.key(acc[k], pos[k]);
-    // Level by level: the keys of [base, base + span] by their bits from `low` on, at most 11; then the bin that holds the cut is
-    // the range, narrowed to what it holds.
-    unsigned base_key = 0, span = ~0u;
-    int low = 21, need = w.keep;
-    bool ties = false;                                   // many equal keys base_key at the cut; else a row stays if ranked >= least
-    unsigned long long least = 0;
     auto ranked = [&](int k) { return (unsigned long long)key[k] << 32 | ~(unsigned)(j0 + k); };
-    auto inside = [&](int k) { return (live >> k & 1u) && key[k] - base_key <= span; };
+    auto inside = [&](const KeyRange& r, int k) { return (live >> k & 1u) && r.holds(key[k]); };
     __syncthreads();
-    for (int level = 0;; ++level) {                      // 21, at most 10, 0
-      if (wave * 64 * R < w.n) {
+    const KeyCut cut = find_cut(
+        w.keep,
+        [&](int level, const KeyRange& r, int need) {
+          if (wave * 64 * R < w.n) {
 #pragma unroll
-        for (int k = 0; k < R; ++k) count_key(hist[level], (int)((key[k] - base_key) >> low), inside(k));
-      }
+            for (int k = 0; k < R; ++k) count_key(hist[level], r.bin_of(key[k]), inside(r, k));
+          }
+          __syncthreads();
+          const Found f = find_bin(hist[level], need, sums, out);
+          return Found{__builtin_amdgcn_readfirstlane(f.bin), __builtin_amdgcn_readfirstlane(f.left), __builtin_amdgcn_readfirstlane(f.count)};
+        },
+        [&](int level, const KeyRange& r, unsigned& smallest, unsigned& largest) {
+          unsigned top = 0, bottom = 0;
+#pragma unroll
+          for (int k = 0; k < R; ++k) {
+            const bool in = inside(r, k);
+            top = max(top, in ? key[k] : 0u);
+            bottom = max(bottom, in ? ~key[k] : 0u);
+          }
+          top = wave_umax(top);
+          bottom = wave_umax(bottom);
+          if (lane == 0) {
+            atomicMax(&ends[level][0], top);
+            atomicMax(&ends[level][1], bottom);
+          }
+          __syncthreads();
+          largest = (unsigned)__builtin_amdgcn_readfirstlane((int)ends[level][0]);
+          smallest = (unsigned)__builtin_amdgcn_readfirstlane((int)~ends[level][1]);
+        });
+    unsigned long long least = (unsigned long long)cut.range.base << 32;         // a row stays if ranked >= least
+    if (!cut.equal && cut.count != cut.need) {           // few: the last to stay is the one that need - 1 of them are larger than
+#pragma unroll
+      for (int k = 0; k < R; ++k)
+        if (inside(cut.range, k)) cand[atomicAdd(&n_cand, 1)] = ranked(k);
       __syncthreads();
-      const Found f = find_bin(hist[level], need, sums, out);
-      base_key = (unsigned)__builtin_amdgcn_readfirstlane((int)(base_key + ((unsigned)f.bin << low)));
-      span = (1u << low) - 1;
-      need = __builtin_amdgcn_readfirstlane(f.left);
-      const int count = __builtin_amdgcn_readfirstlane(f.count);
-      if (count == need) {                               // all of them stay
-        least = (unsigned long long)base_key << 32;
-        break;
-      }
-      if (count <= kRanked) {                            // few: the last to stay is the one that need - 1 of them are larger than
+      constexpr int kParts = kSmallThreads / kRanked;
+      const int i = tid / kParts;
+      const unsigned long long own = i < cut.count ? cand[i] : 0;
+      int larger = 0;
+      for (int c = tid % kParts; c < cut.count; c += kParts) larger += cand[c] > own;
 #pragma unroll
-        for (int k = 0; k < R; ++k)
-          if (inside(k)) cand[atomicAdd(&n_cand, 1)] = ranked(k);
-        __syncthreads();
-        constexpr int kParts = kSmallThreads / kRanked;
-        const int i = tid / kParts;
-        const unsigned long long own = i < count ? cand[i] : 0;
-        int larger = 0;
-        for (int c = tid % kParts; c < count; c += kParts) larger += cand[c] > own;
-#pragma unroll
-        for (int o = kParts / 2; o > 0; o >>= 1) larger += __shfl_xor(larger, o, 64);
-        if (tid % kParts == 0 && i < count && larger == need - 1) bound = own;
-        __syncthreads();
-        least = bound;
-        break;
-      }
-      ties = low == 0;
-      if (ties) break;
-      unsigned top = 0, bottom = 0;
-#pragma unroll
-      for (int k = 0; k < R; ++k) {
-        const bool in = inside(k);
-        top = max(top, in ? key[k] : 0u);
-        bottom = max(bottom, in ? ~key[k] : 0u);
-      }
-      top = wave_umax(top);
-      bottom = wave_umax(bottom);
-      if (lane == 0) {
-        atomicMax(&ends[level][0], top);
-        atomicMax(&ends[level][1], bottom);
-      }
+      for (int o = kParts / 2; o > 0; o >>= 1) larger += __shfl_xor(larger, o, 64);
+      if (tid % kParts == 0 && i < cut.count && larger == cut.need - 1) bound = own;
       __syncthreads();
-      base_key = (unsigned)__builtin_amdgcn_readfirstlane((int)~ends[level][1]);
-      span = (unsigned)__builtin_amdgcn_readfirstlane((int)ends[level][0]) - base_key;
-      ties = span == 0;
-      if (ties) break;
-      low = max(0, 21 - __builtin_clz(span));
+      least = bound;
     }
     unsigned stay = 0;
-    if (!ties) {
+    if (!cut.equal) {
 #pragma unroll
       for (int k = 0; k < R; ++k) stay |= ranked(k) >= least ? 1u << k : 0u;
     } else {
       unsigned tie = 0;
 #pragma unroll
       for (int k = 0; k < R; ++k) {
-        stay |= key[k] > base_key ? 1u << k : 0u;
-        tie |= key[k] == base_key ? 1u << k : 0u;
+        stay |= key[k] > cut.range.base ? 1u << k : 0u;
+        tie |= key[k] == cut.range.base ? 1u << k : 0u;
       }
       tie &= live;
-      int more = need - (int)scan_threads(__popc(tie), wave, tie_sums).before;
+      int more = cut.need - (int)scan_threads(__popc(tie), wave, tie_sums).before;
 #pragma unroll
       for (int k = 0; k < R; ++k) {
         const unsigned one = tie & 1u << k;
