@@ -263,7 +263,10 @@ __global__ __launch_bounds__(kSmallThreads) void evict_small_kernel(EvictParams 
     if (!cut.equal && cut.count != cut.need) {           // few: the last to stay is the one that need - 1 of them are larger than
 #pragma unroll
       for (int k = 0; k < R; ++k)
-        if (inside(cut.range, k)) cand[atomicAdd(&n_cand, 1)] = ranked(k);
+        if (inside(cut.range, k)) {
+          const int at = atomicAdd(&n_cand, 1);
+          if (at < kRanked) cand[at] = ranked(k);        // cut.count of them; the list keeps its size by itself
+        }
       __syncthreads();
       constexpr int kParts = kSmallThreads / kRanked;
       const int i = tid / kParts;
@@ -300,13 +303,13 @@ __global__ __launch_bounds__(kSmallThreads) void evict_small_kernel(EvictParams 
     const unsigned hole = front & ~stay, mover = stay & ~front;
     // 16 bits each: a pair has at most 16384 rows
     const Before b = scan_threads(__popc(hole) | __popc(mover) << 16, wave, move_sums);
-    movers = (int)(b.all >> 16);
+    movers = min((int)(b.all >> 16), (int)(b.all & 0xffffu));           // as many as there are holes; no list is longer
     auto list_rows = [&](int2* list) {
       int at_hole = (int)(b.before & 0xffffu), at_mover = (int)(b.before >> 16);
 #pragma unroll
       for (int k = 0; k < R; ++k) {
-        if (hole >> k & 1u) list[at_hole++].y = j0 + k;
-        if (mover >> k & 1u) list[at_mover++].x = j0 + k;
+        if ((hole >> k & 1u) && at_hole < movers) list[at_hole++].y = j0 + k;
+        if ((mover >> k & 1u) && at_mover < movers) list[at_mover++].x = j0 + k;
       }
     };
     if (p.move_here) list_rows(few);
