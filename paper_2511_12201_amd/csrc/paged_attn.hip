@@ -11,7 +11,9 @@
 //  * Many (paged_tile_kernel): eight wavefronts of 32 query rows share 64-row tiles that go from the pages straight into a ring
 //    of four LDS stages, one barrier a tile; the softmax of a tile runs under the matrix instructions of the next.
 // The weights are rounded to bf16 for the second product (half a step: 2^-8 relative each, the errors of many rows average out);
-// their sum is taken before the rounding, in fp32.
+// their sum is taken before the rounding, in fp32.  Both kernels take the weights against the largest score so far: the weight of a
+// row that stands out is then 1, which bf16 holds, and what one cache row dominates is that row's V.  (A value kept while scores rise
+// leaves 2^x of some fraction x there, rounded above the line and not below: V off by its last bit.)
 #include "paged_dev.h"
 
 #include <type_traits>
@@ -328,8 +330,9 @@ int launch_stream(const AttnParams& p, hipStream_t st) {
 // piece c of row r goes to c ^ (r % 16) (D = 64: c ^ (r / 2 % 8)), so that the 16 lanes that read one piece of 16 rows meet every
 // bank once; V piece c to c ^ 4 (r % 4) (D = 64: c ^ 4 (r / 2 % 2)), so that the transposing reads of 4 rows do.  Ring of four
 // stages, so up to three tiles are in flight while one is computed and one barrier per tile is enough; the waits are counted by hand
-// (the compiler would wait for every load in flight).  2048 tokens of 28 heads on 65536 rows: 1.59 ms, 1.20 PFLOP/s of the 1.34 that
-// a large product reaches; the power limit bounds it (25 calls in a row: 1.68).  Tiles that are not whole (the last one, missing
+// (the compiler would wait for every load in flight).  2048 tokens of 28 heads on 65536 rows: 1.65 ms, 1.16 PFLOP/s of the 1.34 that
+// a large product reaches; of it the maximum in every tile takes 0.08 (of 0.51 ms on 32768 rows of 64 elements 0.02; voted on at the end
+// of a step, not under the second product, 0.04).  Tiles that are not whole (the last one, missing
 // pages) are copied through registers with zeros for what is not there.
 constexpr int kTileWaves = 8, kTileThreads = kTileWaves * 64, kTileRows = kTileWaves * 32;
 constexpr int kTileKeys = 64, kStages = 4;
@@ -384,9 +387,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
     f32x16 o[NB];
 #pragma unroll
     for (int db = 0; db < NB; ++db) o[db] = zero16;
-    float m_run = -INFINITY, l_run = 0.f, mc = 0.f;      // reference value of the weights (mc: times c2, 0 if there is none yet)
-    constexpr float kRescaleSlack = 6.0f;                // it moves when a row exceeds it by this much in the exponent
-    constexpr float kHuge = 1099511627776.f;             // 2^40: fp32 accumulators and bf16 weights are far from their range
+    float m_run = -INFINITY, l_run = 0.f, mc = 0.f;      // the row's largest score so far (mc: times c2, 0 if there is none yet)
 
     // stretches of the span whose table entries fit the window
     const int tiles_per_window = max(1, (int)min((long long)(kTab - 1) << p.pg.shift >> 6, (long long)0x3fffffff));
@@ -485,10 +486,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
           for (int i = 0; i < 16; i += 2) mloc = fmaxf(fmaxf(sn[kb][i], sn[kb][i + 1]), mloc);
         return mloc;
       };
-      auto update_max = [&](float mloc) {
-        mloc = pair_max(mloc);
-        if (__any(mloc > m_run + kRescaleSlack / c2)) rescale(mloc);
-      };
       auto mask_tile = [&](f32x16 (&sn)[2], int t) {
         const int rel = qvis - (c0 + t) * kTileKeys;
         u64 there = ~0ull;
@@ -519,10 +516,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
 
       // One step: weights of tile t from sc and O += V(t) P(t); where there is a tile t + 1, its scores into sn under the
       // weights, and their maximum under the second product.  kSteady: there is one, and tile t + 3 is whole and issued here.
-      // Once every row of the wavefront has a reference value the maximum is not followed any more (kFollow false): the value
-      // can only be too low, and a weight that grows past kHuge shows in the tile's sum.
-      auto step = [&](auto steady, auto follows, f32x16 (&sc)[2], f32x16 (&sn)[2], int t) {
-        constexpr bool kSteady = decltype(steady)::value, kFollow = decltype(follows)::value;
+      auto step = [&](auto steady, f32x16 (&sc)[2], f32x16 (&sn)[2], int t) {
+        constexpr bool kSteady = decltype(steady)::value;
         const bool has_next = kSteady || t + 1 < nt;
         const unsigned stage = (unsigned)(t % kStages) * kStageBytes, stage_n = (unsigned)((t + 1) % kStages) * kStageBytes;
         PFrag pf;
@@ -558,35 +553,32 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
 #pragma unroll
           for (int i = 0; i < 32; i += 2) pf.u[i / 2] = weights(sc, i, lsum);
         }
-        if (__any(lsum > kHuge)) {
-          rescale(pair_max(tile_max(sc)));
-          lsum = 0.f;
-#pragma unroll
-          for (int i = 0; i < 32; i += 2) pf.u[i / 2] = weights(sc, i, lsum);
-        }
         l_run += lsum;
         __builtin_amdgcn_s_setprio(0);
         float mloc = -INFINITY;
-        constexpr int EV = 32 / NPV;
+        constexpr int EV = 64 / NPV;                     // the maximum under the first half of the product, the vote before its end
+        bool higher = false;
 #pragma unroll
         for (int i = 0; i < NPV; ++i) {
           __builtin_amdgcn_sched_barrier(0);
           o[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % kAhead], pf.v[i / NB], o[i % NB], 0, 0, 0);
           if (i + kAhead < NPV) vf[i % kAhead] = vfrag(stage, i + kAhead);
-          if constexpr (kFollow) {
 #pragma unroll
-            for (int e = 0; e < EV; e += 2) {
-              const int x = i * EV + e;
-              mloc = fmaxf(fmaxf(sn[x / 16][x % 16], sn[x / 16][x % 16 + 1]), mloc);
-            }
+          for (int e = 0; i < NPV / 2 && e < EV; e += 2) {
+            const int x = i * EV + e;
+            mloc = fmaxf(fmaxf(sn[x / 16][x % 16], sn[x / 16][x % 16 + 1]), mloc);
           }
+          if (i == NPV * 3 / 4) higher = __any(mloc > m_run);
           if (kSteady && i * LPH % NPV == 0) copy_part(t + 3, i * LPH / NPV, false, from[i * LPH / NPV]);
         }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
         if (has_next) {
-          if (t + 1 >= n_full) mloc = mask_tile(sn, t + 1);
-          if constexpr (kFollow) update_max(mloc);
+          if (t + 1 >= n_full) {
+            mloc = mask_tile(sn, t + 1);
+            higher = __any(mloc > m_run);
+          }
+          if (higher) rescale(pair_max(mloc));
         }
       };
 
@@ -606,19 +598,16 @@ __global__ __launch_bounds__(kTileThreads, 2) void paged_tile_kernel(AttnParams 
         sb[1] = zero16;
 #pragma unroll
         for (int i = 0; i < NQK; ++i) sa[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kfrag(0, i), qf[i / 2], i < 2 ? zero16 : sa[i % 2], 0, 0, 0);
-        update_max(0 >= n_full ? mask_tile(sa, 0) : tile_max(sa));
+        const float first = 0 >= n_full ? mask_tile(sa, 0) : tile_max(sa);
+        if (__any(first > m_run)) rescale(pair_max(first));
         int t = 0;
-        for (; t + 4 < n_plain && __any(m_run == -INFINITY); t += 2) {      // some row has not seen a cache row yet
-          step(std::true_type{}, std::true_type{}, sa, sb, t);
-          step(std::true_type{}, std::true_type{}, sb, sa, t + 1);
-        }
         for (; t + 4 < n_plain; t += 2) {
-          step(std::true_type{}, std::false_type{}, sa, sb, t);
-          step(std::true_type{}, std::false_type{}, sb, sa, t + 1);
+          step(std::true_type{}, sa, sb, t);
+          step(std::true_type{}, sb, sa, t + 1);
         }
         for (; t < nt; t += 2) {
-          step(std::false_type{}, std::true_type{}, sa, sb, t);
-          if (t + 1 < nt) step(std::false_type{}, std::true_type{}, sb, sa, t + 1);
+          step(std::false_type{}, sa, sb, t);
+          if (t + 1 < nt) step(std::false_type{}, sb, sa, t + 1);
         }
       } else {
         for (int t = 0; t + 1 < nt; ++t) {

@@ -12,6 +12,52 @@ from test_gpu_paged import BF16, F32, U32, Cache, Guarded, check_eviction, host,
 pytestmark = pytest.mark.gpu
 
 
+# ------------------------------------------------------------------ attention
+
+@pytest.mark.parametrize("D,rows,n", [(128, 250000, 40), (64, 250000, 40), (128, 9000, 40), (64, 3000, 300), (128, 5000, 9), (128, 90000, 2)])
+def test_what_one_row_dominates_is_its_v(D, rows, n):
+    """Every query row's score on one cache row of its own is 21 to 25, on the others 0: these weigh 250000 exp(-21) < 2e-4 together,
+    so O is that row's V to one rounding, whatever the fraction of the score.  The rows are anywhere among the tiles."""
+    rng = np.random.default_rng(rows + D)
+    H, marks, page_rows = 4, 32, 256
+    cache = Cache(rng, 1, 1, -(-rows // page_rows), page_rows, D, BF16)
+    cache.K.zero_()
+    V = cache.V[cache.table[0, 0].long()].reshape(-1, D)
+    where = np.sort(rng.choice(rows - n, marks, replace=False))
+    for m, j in enumerate(where):
+        cache.K[cache.table[0, 0, j // page_rows].long(), j % page_rows, m] = 1.0
+    mark = rng.integers(0, marks, (H, n))
+    score = rng.uniform(21, 25, (H, n))
+    Q = torch.zeros(1, H, n, D, dtype=BF16, device="cuda")
+    for i, t in itertools.product(range(H), range(n)):
+        Q[0, i, t, mark[i, t]] = float(score[i, t])
+    desc = ob.make_chunk_desc(Q, n_kv_heads=1, softmax_scale=1.0)
+    acc = torch.zeros(1, 1, cache.cap, device="cuda")
+    O, lse = ob.omni_paged_attn(desc, Q, cache.pool, ints([[rows]]), ints([n]), acc_out=acc)
+    z = host(Q.amax(-1))[0]                                  # the scores, exactly
+    seen = rows - n + 1 + np.arange(n)[None]
+    rest = (seen - 1) * np.exp(-z)                            # the others' weights, as shares of the row's
+    v = host(V)[where][mark]                                  # [H, n, D]
+    # the others move O by rest (|v| + 5), their sums are exact to 2^-8; V itself is a bf16 number and may not move a whole step
+    want = v / (1 + rest)[..., None]
+    within(host(O)[0], want, 2.0 ** -9 * np.abs(v) * 1.01 + 2 * rest[..., None] * (np.abs(v) + 6), "O")
+    # score and sum in fp32; 2^x and log2 are off by a few steps.  The sum is 1 and many numbers too small to move it by more than a
+    # step: an addition rounds by up to half a step of 1, 2^-24, for each of the up to 256 spans that share the rows and are joined one
+    # after the other, and for each of the up to 16 tiles of the span, in both halves of a wavefront.
+    within(host(lse)[0], z + np.log1p(rest), 6 * U32 * 25 + 2.0 ** -20 + (256 + 2 * 16) * U32, "lse")
+    p = 1 / (1 + rest)
+    got = host(acc)[0, 0, where]
+    for m, j in enumerate(where):
+        # a weight is off by the roundings of its exponent, 25 log2 e at most, and of the log-sum-exp
+        count = (mark == m).sum()
+        assert abs(got[m] - p[mark == m].sum() - rest_weight(z, seen, mark == m)) <= count * 12 * U32 * 37 + 1e-4
+
+
+def rest_weight(z, seen, own):
+    """What the query rows of the other marks leave on a row: exp(-z) of each, a few 1e-10."""
+    return np.exp(-z[~own]).sum()
+
+
 # ------------------------------------------------------------------ eviction
 
 def border_weights(rng, kind, n, border):
