@@ -694,8 +694,10 @@ int omni_paged_append(const omni_chunk_desc* desc, const omni_rope_desc* rope, c
  *   Q [batch, n_q_heads, n_new, head_dim], O the same shape and strides
  *   lse [batch, n_q_heads, n_new] f32, out
  *   page_rows at least 16
- * bf16: both products on the bf16 matrix cores (the probabilities rounded to bf16 for the
- * second), sums in fp32; fp32: fp32 matrix cores.
+ * bf16: both products on the bf16 matrix cores, sums in fp32.  For the second the probabilities
+ * are two bf16 numbers each (17 bits) where a pair has at most 32 query rows (n_new *
+ * n_q_heads / n_kv_heads), else one (8 bits, relative to the largest so far: what one cache
+ * row dominates is that row's V).  fp32: fp32 matrix cores.
  * Workspace: OMNI_CALL_PAGED_ATTN with param = rows_cap where acc_out is given, else 0.
  */
 int omni_paged_attn(const omni_chunk_desc* desc, const void* Q, const omni_page_pool* pool,

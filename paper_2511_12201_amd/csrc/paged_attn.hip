@@ -10,8 +10,9 @@
 //    cache of its own through LDS; the states of a workgroup's wavefronts meet at an item's end.
 //  * Many (paged_tile_kernel): eight wavefronts of 32 query rows share 64-row tiles that go from the pages straight into a ring
 //    of four LDS stages, one barrier a tile; the softmax of a tile runs under the matrix instructions of the next.
-// The weights are rounded to bf16 for the second product (half a step: 2^-8 relative each, the errors of many rows average out);
-// their sum is taken before the rounding, in fp32.  Both kernels take the weights against the largest score so far: the weight of a
+// The second product takes a weight as two bf16 numbers (17 bits) where memory bounds it, and as one where the matrix instructions do
+// (half a step: 2^-8 relative, the errors of many rows average out; two would cost 56 % of 2048 tokens on 65536 rows).  Their sum is
+// taken before the rounding, in fp32.  Both kernels take the weights against the largest score so far: the weight of a
 // row that stands out is then 1, which bf16 holds, and what one cache row dominates is that row's V.  (A value kept while scores rise
 // leaves 2^x of some fraction x there, rounded above the line and not below: V off by its last bit.)
 #include "paged_dev.h"
@@ -232,9 +233,13 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
       }
-      union { bf16x8 v[2]; unsigned u[8]; } pf;
+      // a weight as two bf16 numbers: the matrix cores have the time here (one token of eight sequences on 131089 rows 325 / 327 us)
+      union { bf16x8 v[2]; unsigned u[8]; } pf, rest;
 #pragma unroll
-      for (int i = 0; i < 16; i += 2) pf.u[i / 2] = pack_bf16x2(s[i], s[i + 1]);
+      for (int i = 0; i < 16; i += 2) {
+        const unsigned u = pf.u[i / 2] = pack_bf16x2(s[i], s[i + 1]);
+        rest.u[i / 2] = pack_bf16x2(s[i] - __uint_as_float(u << 16), s[i + 1] - __uint_as_float(u & 0xffff0000u));
+      }
       // V of this block has landed: newer are the next block, the K after it and this trip's stores
       if (next2) wait_vmcnt<3 * LPH + kStores>();
       else if (next) wait_vmcnt<2 * LPH>();
@@ -254,6 +259,10 @@ __global__ __launch_bounds__(kStreamThreads, 1) void paged_stream_kernel(AttnPar
       for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
         for (int db = 0; db < NB; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s2][db].v, pf.v[s2], o[db], 0, 0, 0);
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+        for (int db = 0; db < NB; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s2][db].v, rest.v[s2], o[db], 0, 0, 0);
       row_a = row_a1;
       row_b = row_b1;
       row_a1 = row_a2;

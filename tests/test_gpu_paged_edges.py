@@ -58,6 +58,29 @@ def rest_weight(z, seen, own):
     return np.exp(-z[~own]).sum()
 
 
+def exact_scores(rng, cache, Q):
+    """Q and K of -1, 0 and 1: a score is a whole number, whatever order its sum is taken in."""
+    cache.K.copy_(torch.from_numpy(rng.integers(-1, 2, cache.K.shape).astype(np.float32)))
+    Q.copy_(torch.from_numpy(rng.integers(-1, 2, Q.shape).astype(np.float32)))
+
+
+@pytest.mark.parametrize("H,n,rows", [(7, 1, 60), (7, 4, 200), (32, 1, 300), (1, 32, 90), (3, 2, 17)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_weights_of_few_query_rows_keep_17_bits(H, n, rows, D):
+    rng = np.random.default_rng(rows)
+    cache = Cache(rng, 1, 1, -(-rows // 16), 16, D, BF16)
+    Q = torch.zeros(1, H, n, D, dtype=BF16, device="cuda")
+    exact_scores(rng, cache, Q)
+    desc = ob.make_chunk_desc(Q, n_kv_heads=1, softmax_scale=0.25)
+    O, lse = ob.omni_paged_attn(desc, Q, cache.pool, ints([[rows]]), ints([n]))
+    wO, wl, _, pv, qk = po.attend(host(Q), cache.oracle(), np.array([[rows]]), [n], True, 0.25)
+    # exponents below 32 log2 e with two roundings, 2^x off by 2^-22, `rows` additions in numerator and sum; a weight as two
+    # numbers of 8 bits is off by 2^-17; half a step of the output
+    e = 2 * (2 * 47 * U32 + 2.0 ** -22) + 2 * rows * U32 + 2.0 ** -17
+    within(host(O), wO, e * pv + 2.0 ** -8 * np.abs(wO), "O")
+    within(host(lse), wl, 2 * (2 * 47 * U32 + 2.0 ** -22) + rows * U32 + 4 * U32 * np.abs(wl), "lse")
+
+
 # ------------------------------------------------------------------ eviction
 
 def border_weights(rng, kind, n, border):
