@@ -691,6 +691,8 @@ int omni_paged_append(const omni_chunk_desc* desc, const omni_rope_desc* rope, c
  * the KV head and over the new tokens of the attention probabilities):
  *   acc_out[b, g, j] = acc_in[b, g, j] + sum p[j]     for j < row_end[b, g]
  * acc_in null counts as zeros; acc_in may be acc_out; both null: no weights.  16-byte aligned.
+ * A NaN among the scores that a token sees makes its O and lse and the weights of the rows it
+ * sees NaN; other tokens and other rows keep their values.
  *   Q [batch, n_q_heads, n_new, head_dim], O the same shape and strides
  *   lse [batch, n_q_heads, n_new] f32, out
  *   page_rows at least 16

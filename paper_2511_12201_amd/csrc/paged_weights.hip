@@ -323,12 +323,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_weights_bf16_kernel(AttnPar
       __builtin_amdgcn_sched_barrier(0);
       const float lse = sLse[stage][wave][qb * 32 + ln];
       ref = lse * kLog2e;
-      if ((tile + 1) * kBfQ > w.M || lse == -INFINITY) {          // behind the last row, or a row that sees nothing
-        const int r = tile * kBfQ + qb * 32 + ln;
-        if (r >= w.M || lse == -INFINITY) {
+      if ((tile + 1) * kBfQ > w.M || !(lse > -INFINITY)) {
+        // behind the last row, or a row that sees nothing: no weights; NaN: a NaN for every row that is not masked below
+        const bool none = tile * kBfQ + qb * 32 + ln >= w.M || lse == -INFINITY;
+        if (none || lse != lse) {
           ref = 0.f;
 #pragma unroll
-          for (int x = 0; x < 32; ++x) s[x / 16][x % 16] = -INFINITY;
+          for (int x = 0; x < 32; ++x) s[x / 16][x % 16] = none ? -INFINITY : lse;
         }
       }
       if (tile < clear) {
@@ -432,7 +433,7 @@ __global__ __launch_bounds__(kThreads) void paged_weights_logits_kernel(AttnPara
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[k][e] += fast_exp2(x[k][e] - ref);
+      for (int e = 0; e < 4; ++e) sum[k][e] += x[k][e] == -INFINITY ? 0.f : fast_exp2(x[k][e] - ref);     // not seen: 0 whatever the token's sum is
   }
   f32x4 mine = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll

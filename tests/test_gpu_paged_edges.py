@@ -81,6 +81,33 @@ def test_weights_of_few_query_rows_keep_17_bits(H, n, rows, D):
     within(host(lse), wl, 2 * (2 * 47 * U32 + 2.0 ** -22) + rows * U32 + 4 * U32 * np.abs(wl), "lse")
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,end", [(3, 70), (10, 430), (40, 430), (300, 430), (600, 900)])
+def test_a_nan_token_leaves_the_rows_it_does_not_see_alone(dtype, n, end):
+    """One query row of one token is NaN: the weights of the rows that it sees are, those behind them and on a page that is missing are
+    what they were without it."""
+    rng = np.random.default_rng(n)
+    cache = Cache(rng, 1, 1, -(-end // 16), 16, 64, dtype)
+    cache.table[0, 0, 1] = -1
+    Q = rand(rng, 1, 3, n, 64, dtype=dtype)
+    desc, token = ob.make_chunk_desc(Q, n_kv_heads=1), n // 2
+    out = []
+    for value in (None, float("nan")):
+        if value is not None:
+            Q[0, 1, token, 7] = value
+        acc = torch.full((1, 1, cache.cap), 0.5, device="cuda")
+        out.append((*ob.omni_paged_attn(desc, Q, cache.pool, ints([[end]]), ints([n]), acc_in=acc, acc_out=acc), acc[0, 0]))
+    (O, lse, acc), (bad_O, bad_lse, bad) = out
+    seen = end - n + token + 1
+    there = torch.arange(cache.cap, device="cuda") // 16 != 1
+    assert bad[:seen][there[:seen]].isnan().all() and (bad[:end][~there[:end]] == 0.5).all() and (bad[end:] == 0.5).all()
+    assert torch.equal(bad[seen:], acc[seen:])               # the other tokens' weights, in the same order
+    assert bad_O[0, 1, token].isnan().all() and bad_lse[0, 1, token].isnan()
+    clean = torch.ones(3, n, dtype=torch.bool, device="cuda")
+    clean[1, token] = False
+    assert torch.equal(bad_O[0][clean], O[0][clean]) and torch.equal(bad_lse[0][clean], lse[0][clean])
+
+
 # ------------------------------------------------------------------ eviction
 
 def border_weights(rng, kind, n, border):
