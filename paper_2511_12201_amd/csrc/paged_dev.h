@@ -210,6 +210,33 @@ __device__ __forceinline__ void for_segments(const AttnParams& p, Scan& s, F f) 
   }
 }
 
+// S^T = K Q^T of 32 cache rows and 32 query rows in fp32.  A 32x32x2 instruction adds two products to every score, element e of the lane
+// halves' elements [h D/2, (h + 1) D/2).  A score is a sum of sums of 32 products: one chain of D/2 additions rounds as often at the
+// size of the whole (one token on 3370 rows of 128 elements: 1.2e-6 of the output's norm, so 5.3e-7; 256 tokens on 8192 rows 263 / 268 us,
+// with weights 421 / 436).  Attention and weights form their
+// scores here, so that a weight and the log-sum-exp that it is taken against are of the same scores.
+//   operands(e, k, q): elements e .. e + 3 of the lane's half
+template <int D, typename F>
+__device__ __forceinline__ f32x16 scores_f32(F operands) {
+  constexpr int kChain = 16;
+  f32x16 total, part;
+#pragma unroll
+  for (int e0 = 0; e0 < D / 2; e0 += kChain) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) part[i] = 0.f;
+#pragma unroll
+    for (int e = e0; e < e0 + kChain; e += 4) {
+      f32x4 k, q;
+      operands(e, k, q);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) part = __builtin_amdgcn_mfma_f32_32x32x2f32(k[x], q[x], part, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) total[i] = e0 ? total[i] + part[i] : part[i];
+  }
+  return total;
+}
+
 // Output row r of a pair and its place in the log-sum-exps.
 __device__ __forceinline__ long long out_row(const AttnParams& p, const PairView& w, int r, long long& at_lse) {
   const int t = r / p.c.G, head = w.g * p.c.G + r % p.c.G;

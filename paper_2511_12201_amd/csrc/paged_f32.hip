@@ -5,7 +5,7 @@
 // B operand as they stand (register i holds row 8 (i / 4) + 4 h + i % 4).  Two divisions of labour: four wavefronts of 32 query rows
 // that share 32-row tiles of the cache, or, for pairs of at most 32 query rows, four wavefronts that take 32-row tiles of their own
 // and join their states.  The matrix instructions bound it (64 cycles each, D of them per 32 x 32 tile): 256 tokens of 28 heads on 8192
-// rows of 128 elements 265 us, 113 TFLOP/s of the 154 that a large product reaches.
+// rows of 128 elements 268 us, 112 TFLOP/s of the 154 that a large product reaches.
 #include "paged_dev.h"
 
 namespace omni {
@@ -20,9 +20,6 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 1 : 2) void paged_attn_f32_kernel
   constexpr int PITCH = D + 4, TILE = 32 * PITCH, NB = D / 32;
   constexpr int LOADERS = SPLIT ? 64 : kThreads;         // threads that stage a tile
   constexpr int CPR = D / 4, NL = 32 * CPR / LOADERS;    // 16-byte pieces of a row, of a tile per loader
-  // A score as four sums where the registers allow it: 64 roundings of one sum put 1.2e-6 of its norm into the output of one token on
-  // 3370 rows, four sums of 16 5.3e-7.
-  constexpr int SUMS = SPLIT || D == 64 ? 4 : 1;
   __shared__ __attribute__((aligned(16))) float sK[(SPLIT ? kWaves : 1) * TILE], sV[(SPLIT ? kWaves : 1) * TILE];
   __shared__ Scan scan;
   __shared__ float sM[kWaves][32], sL[kWaves][32];
@@ -89,19 +86,10 @@ __global__ __launch_bounds__(kThreads, SPLIT ? 1 : 2) void paged_attn_f32_kernel
       const unsigned there = there_next >> (4 * h);
       __syncthreads();
       if (tile + step < last) fetch(j0 + 32 * step);
-      f32x16 s, sums[SUMS];
-#pragma unroll
-      for (int x = 0; x < SUMS; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sums[x][i] = 0.f;
-#pragma unroll
-      for (int k = 0; k < D / 2; k += 4) {
-        const f32x4 kv = *reinterpret_cast<const f32x4*>(tk + ln * PITCH + h * (D / 2) + k);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sums[e % SUMS] = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[e], q[k + e], sums[e % SUMS], 0, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = SUMS == 4 ? (sums[0][i] + sums[1 % SUMS][i]) + (sums[2 % SUMS][i] + sums[3 % SUMS][i]) : sums[0][i];
+      f32x16 s = scores_f32<D>([&](int e, f32x4& kv, f32x4& qv) {
+        kv = *reinterpret_cast<const f32x4*>(tk + ln * PITCH + h * (D / 2) + e);
+        qv = f32x4{q[e], q[e + 1], q[e + 2], q[e + 3]};
+      });
       float mx = m;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {

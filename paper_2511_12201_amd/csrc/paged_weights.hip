@@ -179,15 +179,10 @@ __global__ __launch_bounds__(kThreads) void paged_weights_f32_kernel(AttnParams 
       }
       __syncthreads();
       if (tile + 1 < seg.t1) load((tile + 1) * 32);
-      f32x16 s;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-      for (int e = 0; e < D / 2; e += 4) {
-        const f32x4 q = *reinterpret_cast<const f32x4*>(sQ + ln * PITCH + h * (D / 2) + e);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e + x], q[x], s, 0, 0, 0);
-      }
+      const f32x16 s = scores_f32<D>([&](int e, f32x4& kv, f32x4& qv) {
+        kv = f32x4{k[e], k[e + 1], k[e + 2], k[e + 3]};
+        qv = *reinterpret_cast<const f32x4*>(sQ + ln * PITCH + h * (D / 2) + e);
+      });
       const int vis = sVis[ln];
       const float ref = sL[ln];
 #pragma unroll

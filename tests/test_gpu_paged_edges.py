@@ -81,6 +81,29 @@ def test_weights_of_few_query_rows_keep_17_bits(H, n, rows, D):
     within(host(lse), wl, 2 * (2 * 47 * U32 + 2.0 ** -22) + rows * U32 + 4 * U32 * np.abs(wl), "lse")
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [1, 30, 200])
+def test_an_fp32_score_is_a_sum_of_short_sums(D, n):
+    """A product of 1 and D - 1 of just over a quarter of a step of 1: added to the 1 one by one they are lost, by pairs each rounds up, so
+    that one chain is off by about D / 4 steps of 1.  One row is seen: its log-sum-exp is the score, its weight 1 a query row."""
+    rng = np.random.default_rng(0)
+    small = 0.51 * 2.0 ** -24
+    cache = Cache(rng, 1, 1, 1, 16, D, F32)
+    cache.K.fill_(2.0 ** -12)
+    Q = torch.full((1, 2, n, D), small * 2.0 ** 12, device="cuda")
+    Q[..., 0], cache.K[..., 0] = 1.0, 1.0
+    desc = ob.make_chunk_desc(Q, n_kv_heads=1, causal=False, softmax_scale=1.0)
+    acc = torch.zeros(1, 1, 16, device="cuda")
+    O, lse = ob.omni_paged_attn(desc, Q, cache.pool, ints([[1]]), ints([n]), acc_out=acc)
+    # 31 small products are added to the 1, each off by no more than itself (one by one: lost) or by half a step for each pair; three
+    # additions of the sums round by half a step; the exponent's and the logarithm's scale are two products with rounded constants
+    bar = (31 * 0.51 + 3 + 5) * 2.0 ** -24
+    within(host(lse), 1 + (D - 1) * small, bar, "lse")
+    # the same scores in the weights: what is left is the rounding of their logarithms' scale, and 2 n ones are added
+    assert abs(float(acc[0, 0, 0]) - 2 * n) <= 2 * n * (8 + 2 * n) * 2.0 ** -24
+    assert torch.equal(O, cache.V[cache.table[0, 0, 0].long(), 0].expand_as(O))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("n,end", [(3, 70), (10, 430), (40, 430), (300, 430), (600, 900)])
 def test_a_nan_token_leaves_the_rows_it_does_not_see_alone(dtype, n, end):
