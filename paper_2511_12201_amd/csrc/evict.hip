@@ -344,15 +344,15 @@ __device__ __forceinline__ int* chunk_coarse(const EvictParams& p, int d, int pa
   return p.coarse + (((long long)d * gridDim.y + pair) * kChunks + c) * 64;
 }
 
-// The bin of digit d that holds the need-th largest key, how many of it are wanted, and whether that is all of it, from the chunks'
-// histograms: the 32 bins first that hold it, then the bin.  (All bins of all chunks are 320 KB a workgroup: 12.5 us for a launch of
-// 320 workgroups that takes 6 so.)  Wavefront v reads chunks v, v + 8, .. and keeps their counts: with them it knows how many keys of
+// The bin of digit d that holds the need-th largest key, and how many of it are wanted, from the chunks' histograms: the 32 bins first
+// that hold it, then the bin.  (All bins of all chunks are 320 KB a workgroup: 12.5 us for a launch of 320 workgroups that takes 6
+// so.)  Wavefront v reads chunks v, v + 8, .. and keeps their counts: with them it knows how many keys of
 // such a chunk lie above the bin.  All threads call `find`.
 struct DigitCut {
   static constexpr int kWaves = kChunkThreads / 64, kOwn = kChunks / kWaves;
   static_assert(kOwn * kWaves == kChunks && kFine == 32, "");
   int wide[kOwn], fine[(kOwn + 1) / 2];                  // fine: chunk k of the wavefront in lanes 32 (k % 2) .. + 31
-  Found f;
+  int bin, left;
   __device__ __forceinline__ void find(const EvictParams& p, int d, int pair, int need, int (*part)[64]) {
     const int lane = lane_id(), wave = threadIdx.x >> 6;
     int s = 0;
@@ -387,15 +387,13 @@ struct DigitCut {
     if (lane >= 32) n = 0;
     inc = (int)wave_scan((unsigned)n);
     at = __ffsll((unsigned long long)__ballot(inc >= need)) - 1;
-    const int all = __shfl(n, at, 64);
-    f.left = need - __shfl(inc - n, at, 64);
-    f.bin = group * kFine + 31 - at;
-    f.count = all;
+    left = need - __shfl(inc - n, at, 64);
+    bin = group * kFine + 31 - at;
   }
   // keys above the bin of the wavefront's chunk k, and in it
   __device__ __forceinline__ int2 chunk(int k) const {
-    const int lane = lane_id(), at = f.bin % kFine;
-    const int n = (lane > f.bin / kFine ? wide[k] : 0) + (lane / 32 == k % 2 && lane % 32 > at ? fine[k / 2] : 0);
+    const int lane = lane_id(), at = bin % kFine;
+    const int n = (lane > bin / kFine ? wide[k] : 0) + (lane / 32 == k % 2 && lane % 32 > at ? fine[k / 2] : 0);
     return int2{(int)__shfl(wave_scan((unsigned)n), 63, 64), __shfl(fine[k / 2], k % 2 * 32 + at, 64)};
   }
 };
@@ -428,10 +426,10 @@ __global__ __launch_bounds__(kChunkThreads) void evict_digit_kernel(EvictParams 
     const int so_far = D == 1 ? 0 : p.above[pair * kChunks + blockIdx.x];
     DigitCut digit;
     digit.find(p, D - 1, pair, need, part);
-    prefix = with_digit(prefix, digit.f.bin, D - 1);
+    prefix = with_digit(prefix, digit.bin, D - 1);
     if (blockIdx.x == 0 && tid == 0) {                   // for the next launch; digits of different launches do not meet
       p.cut[pair * 4 + (D == 1 ? 0 : 2)] = (int)prefix;
-      p.cut[pair * 4 + (D == 1 ? 1 : 3)] = digit.f.left;
+      p.cut[pair * 4 + (D == 1 ? 1 : 3)] = digit.left;
     }
 #pragma unroll
     for (int k = 0; k < DigitCut::kOwn; ++k) {           // keys of this chunk above the bin
@@ -496,8 +494,8 @@ __global__ __launch_bounds__(kChunkThreads) void evict_lists_kernel(EvictParams 
   for (int k = 0; k < DigitCut::kOwn; ++k) higher[k] = p.above[pair * kChunks + wave + k * kWaves];
   DigitCut digit;
   digit.find(p, 2, pair, p.cut[pair * 4 + 3], part);
-  const unsigned cut = with_digit((unsigned)p.cut[pair * 4 + 2], digit.f.bin, 2);
-  const int need = digit.f.left;
+  const unsigned cut = with_digit((unsigned)p.cut[pair * 4 + 2], digit.bin, 2);
+  const int need = digit.left;
 #pragma unroll
   for (int k = 0; k < DigitCut::kOwn; ++k) {
     const int2 n = digit.chunk(k);
