@@ -668,7 +668,12 @@ int omni_rope(const omni_rope_desc* rope, const omni_layer_desc* desc, const voi
  * omni_paged_append -- new token t < new_cnt[b] of sequence b, at position pos[b] + t, is
  * stored as row row_cnt[b, g] + t of every KV head g: K turned by rope (null: as it is), V,
  * row_pos, and acc = 0 (acc may be null).  row_end[b, g] = row_cnt[b, g] + new_cnt[b]
- * (rows_cap at most; rows that do not fit are dropped).  With rope, Q is turned too:
+ * (rows_cap at most; rows that do not fit are dropped).  Keep row_cnt + new_cnt within rows_cap
+ * (evict first): row_end does not tell how many rows were dropped, and omni_paged_attn with
+ * the same new_cnt takes the last rows for the chunk's, so that every token of a sequence
+ * that ran over sees that many rows fewer than it should.  Where all pairs of a sequence hold
+ * equally many rows, new_cnt = rows_cap - row_cnt in the attention gives the tokens that
+ * were stored theirs, and the dropped ones O = 0.  With rope, Q is turned too:
  *   Q [batch, n_q_heads, n_new, head_dim] -> Qout, same strides, may be Q itself; rows
  *   t >= new_cnt[b] are not written.  Without rope both must be null.
  *   K, V [batch, n_kv_heads, n_new, head_dim]; pos, new_cnt [batch] i32
@@ -681,7 +686,8 @@ int omni_paged_append(const omni_chunk_desc* desc, const omni_rope_desc* rope, c
 
 /*
  * omni_paged_attn -- attention of a chunk of new tokens over the pages, one token to many.
- * The chunk's own rows are the last new_cnt[b] of the row_end[b, g] rows of a pair, so new
+ * The chunk's own rows are the last new_cnt[b] of the row_end[b, g] rows of a pair (all of
+ * them stored: see above for a chunk that omni_paged_append could not place), so new
  * token t sees rows [0, row_end - new_cnt + t] (causal) or all of them:
  *   O = softmax(q . K^T softmax_scale) V,  lse = log sum exp of the scaled products.
  * A token that sees no row, and t >= new_cnt[b], get O = 0 and lse = -inf.  Q of the

@@ -1023,7 +1023,8 @@ def omni_rope(rope: RopeDesc, desc: LayerDesc, Q, K, pos=None, backward: bool = 
 def omni_paged_append(desc: ChunkDesc, rope: RopeDesc | None, Q, K, V, pool: PagePool, pos, new_cnt, row_cnt, row_pos, acc=None,
                       Qout=None, row_end=None):
     """Store a chunk's K (turned) and V behind the rows of its pages and turn its Q: (Qout, row_end).  Without rope Q is None
-    and K is stored as it is.  row_pos and acc [B, Hkv, rows_cap] get the new rows' positions and zeros."""
+    and K is stored as it is.  row_pos and acc [B, Hkv, rows_cap] get the new rows' positions and zeros.  Rows beyond rows_cap
+    are dropped, and the attention of such a chunk is not this new_cnt's (the header says whose): evict first."""
     dev, dt = K.device, _DTYPES[desc.dtype]
     B, Hkv, n, D = desc.batch, desc.n_kv_heads, desc.n_new, desc.head_dim
     ks = (*desc.kv_stride, 1)

@@ -7,7 +7,7 @@ import torch
 
 from oracle import paged_oracle as po
 from paper_2511_12201_amd import binding as ob
-from test_gpu_paged import BF16, F32, U32, Cache, Guarded, check_eviction, host, ints, rand, within
+from test_gpu_paged import BF16, F32, U32, Cache, Guarded, check_attention, check_eviction, host, ints, rand, within
 
 pytestmark = pytest.mark.gpu
 
@@ -129,6 +129,30 @@ def test_a_nan_token_leaves_the_rows_it_does_not_see_alone(dtype, n, end):
     clean = torch.ones(3, n, dtype=torch.bool, device="cuda")
     clean[1, token] = False
     assert torch.equal(bad_O[0][clean], O[0][clean]) and torch.equal(bad_lse[0][clean], lse[0][clean])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [6, 40])
+def test_attention_after_an_append_that_ran_over(dtype, n):
+    """Sequence 0 has room for 4 of its tokens: with the counts of what was stored these see what they should and the others nothing;
+    sequence 1, which fits, is not affected."""
+    rng = np.random.default_rng(n)
+    cache = Cache(rng, 2, 2, 8, 16, 64, dtype)
+    Q, K, V = (rand(rng, 2, h, n, 64, dtype=dtype) for h in (4, 2, 2))
+    cap, pos = cache.cap, torch.zeros(2, 2, cache.cap, dtype=torch.int32, device="cuda")
+    have = [cap - 4, 20]
+    _, end = ob.omni_paged_append(ob.make_chunk_desc(Q, K), None, None, K, V, cache.pool, ints(have), ints([n, n]),
+                                  ints([[h, h] for h in have]), pos)
+    assert end.tolist() == [[cap, cap], [20 + n, 20 + n]]
+    stored = [min(n, cap - h) for h in have]
+    O, lse, _ = check_attention(cache, Q, end.tolist(), stored, True, True, dtype)
+    assert not O[0, :, 4:].any() and torch.isneginf(lse[0, :, 4:]).all()
+    # the oracle on sequence 0 with the rows that it had and each stored token's own behind them, one token at a time
+    pool = cache.oracle()
+    for t in range(4):
+        wO, _, _, pv, qk = po.attend(host(Q[:1, :, t:t + 1]), pool, np.full((1, 2), have[0] + t + 1), [1], False, 0.125)
+        bar = (2 * ((64 + 2) * U32 * qk + 2.0 ** -21) + 2 * cap * U32)[..., None] * pv + (2 * 2.0 ** -8 * pv + 2.0 ** -8 * np.abs(wO)) * (dtype is BF16) + U32
+        within(host(O[:1, :, t:t + 1]), wO, bar, f"token {t}")
 
 
 # ------------------------------------------------------------------ eviction
