@@ -715,12 +715,15 @@ int omni_paged_attn(const omni_chunk_desc* desc, const void* Q, const omni_page_
 /*
  * omni_paged_evict -- per pair the min(row_end, budget) rows that stay: those spared by
  * their position (row_pos < n_sink, or row_pos >= seq_len[b] - n_recent) before all others,
- * then those of largest acc (NaN below everything); equal ones by lowest row.  The rows
+ * then those of largest acc (NaN counts as -inf); equal ones by lowest row.  The rows
  * that stay move together without keeping their order: of the rows that leave, those in
  * front of the new end are holes, and the k-th hole takes the k-th staying row from
  * behind the new end.  Only those rows are copied (K, V in the pages; the attention of
  * later tokens does not depend on the order of the rows), and a page behind the new end is
  * free afterwards.
+ * A row on a page that is not there is ranked like any other; if it moves, or a row moves to
+ * such a page, position and weight do and K and V do not: have the pages of all rows in use in
+ * the table.
  *   desc    batch, n_kv_heads, head_dim and dtype are used
  *   budget  rows per pair, >= 1 and >= n_sink + n_recent; n_sink, n_recent >= 0
  *   seq_len [batch] i32: the position after the last token

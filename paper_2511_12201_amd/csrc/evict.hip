@@ -1,7 +1,7 @@
 // Eviction from a paged cache by accumulated attention weight (omni_paged_evict).
 //
-// Per (sequence, KV head) pair the rows are ranked by a 32-bit key (spared rows above every weight, the weights in order, NaN
-// below them) and the `keep` largest stay, equal keys by lowest row.  The key at the cut is found by histograms in LDS of 11 bits
+// Per (sequence, KV head) pair the rows are ranked by a 32-bit key (spared rows above every weight, the weights in order, NaN as
+// -inf) and the `keep` largest stay, equal keys by lowest row.  The key at the cut is found by histograms in LDS of 11 bits
 // of the keys at a time; then the rows are counted in order, which splits the ties and numbers the holes and the rows that move into
 // them.  Rows are only copied where they have to: a row that stays in front of the new end stays where it is.
 //
