@@ -7,7 +7,7 @@ import torch
 
 from oracle import paged_oracle as po
 from paper_2511_12201_amd import binding as ob
-from test_gpu_paged import BF16, F32, U32, Cache, Guarded, check_attention, check_eviction, host, ints, rand, within
+from test_gpu_paged import BF16, F32, U32, Cache, Guarded, attend_bars, check_attention, check_eviction, host, ints, rand, within
 
 pytestmark = pytest.mark.gpu
 
@@ -153,6 +153,83 @@ def test_attention_after_an_append_that_ran_over(dtype, n):
         wO, _, _, pv, qk = po.attend(host(Q[:1, :, t:t + 1]), pool, np.full((1, 2), have[0] + t + 1), [1], False, 0.125)
         bar = (2 * ((64 + 2) * U32 * qk + 2.0 ** -21) + 2 * cap * U32)[..., None] * pv + (2 * 2.0 ** -8 * pv + 2.0 ** -8 * np.abs(wO)) * (dtype is BF16) + U32
         within(host(O[:1, :, t:t + 1]), wO, bar, f"token {t}")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("G,n,end,page_rows,D", [
+    (1, 1, 700, 16, 64), (7, 1, 9001, 64, 128), (4, 8, 5003, 32, 64), (4, 9, 4000, 16, 128), (7, 40, 33001, 16, 128), (2, 130, 8321, 256, 64),
+    (1, 300, 300, 64, 128), (3, 257, 2050, 16, 64), (8, 64, 66000, 16, 64)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_every_row_counts_once(G, n, end, page_rows, D, causal, dtype):
+    """All scores are 0: every weight is 1, sums are whole numbers, the log-sum-exp is the logarithm of the number of rows seen.  Column
+    c of V marks up to 32 rows of the cache, the first and last of its tiles and windows before others: O times the number of
+    rows is how many of them a token sees, and 1 / 32 of that is far above a bf16 rounding."""
+    rng = np.random.default_rng(end)
+    Hkv, B = 2, 1
+    cache = Cache(rng, B, Hkv, -(-end // page_rows), page_rows, D, dtype)
+    cache.K.zero_()
+    cache.V.zero_()
+    ends = [end, end - 13]
+    j = np.arange(end)
+    border = np.flatnonzero((j % 64 < 2) | (j % 64 > 61) | (j % 32 == 0) | (j % 32 == 31))
+    first = np.concatenate([rng.permutation(border), rng.permutation(np.setdiff1d(j, border))])[:32 * D]
+    column = np.full(end, -1)
+    column[first] = np.arange(len(first)) % D
+    table = cache.table.cpu().numpy()
+    for g in range(Hkv):
+        at = torch.from_numpy(table[0, g, first // page_rows].astype(np.int64)).cuda()
+        cache.V[at, torch.from_numpy(first % page_rows).cuda(), torch.from_numpy(column[first]).cuda()] = 1.0
+    cache.poison([ends])
+    Q = rand(rng, B, Hkv * G, n, D, dtype=dtype)
+    acc = torch.zeros(B, Hkv, cache.cap, device="cuda")
+    O, lse = ob.omni_paged_attn(ob.make_chunk_desc(Q, n_kv_heads=Hkv, causal=causal), Q, cache.pool, ints([ends]), ints([n]), acc_out=acc)
+    for g, e in enumerate(ends):
+        seen = np.maximum(e - n + 1 + np.arange(n), 0) if causal else np.full(n, e)
+        marks = np.zeros((end + 1, D))
+        marks[1:][first, column[first]] = 1
+        count = marks.cumsum(0)[seen]                                # [n, D] marked rows that a token sees
+        heads = slice(g * G, (g + 1) * G)
+        want = count / np.maximum(seen, 1)[:, None]
+        # 1 / sum, the product with it, the store
+        within(host(O)[0, heads], np.broadcast_to(want, (G, n, D)), want * ((2.0 ** -8 if dtype is BF16 else U32) + 3 * U32), "O")
+        with np.errstate(divide="ignore"):
+            log = np.log(seen.astype(np.float64))
+        # log2 off by four steps of its size, times a rounded constant
+        within(host(lse)[0, heads], np.broadcast_to(log, (G, n)), 6 * 2 * U32 * np.abs(np.where(seen > 0, log, 0)), "lse")
+        share = np.where(seen > 0, G / np.maximum(seen, 1), 0.0)
+        w = np.zeros(e)
+        for t in range(n):
+            w[:seen[t]] += share[t]
+        # an exponent below 17 with three roundings, 2^x off by 2^-22, G n additions
+        within(host(acc)[0, g, :e], w, (3 * 2 * 17 * U32 + 2.0 ** -21 + G * n * U32) * w, "weights")
+
+
+TIGHT = [((28, 4), 128, 1, 64, 700, True), ((8, 2), 128, 9, 16, 64, True), ((4, 2), 128, 40, 16, 100, True), ((28, 4), 128, 37, 64, 257, True),
+         ((6, 1), 64, 90, 32, 511, True), ((8, 2), 128, 70, 128, 300, False), ((40, 1), 64, 2, 16, 77, True), ((3, 3), 128, 260, 64, 300, True)]
+
+
+@pytest.mark.parametrize("shape", TIGHT, ids=str)
+def test_sums_of_bf16_attention_are_fp32_sums(shape):
+    """Products of bf16 numbers are exact in fp32: log-sum-exps and weights, which are never rounded to bf16, keep to the bars of fp32."""
+    heads, D, n, page_rows, end, causal = shape
+    rng = np.random.default_rng(end + 1)
+    (H, Hkv), ends = heads, [[end - 3 * g for g in range(heads[1])]]
+    cache = Cache(rng, 1, Hkv, -(-end // page_rows), page_rows, D, BF16)
+    cache.poison(ends)
+    Q = rand(rng, 1, H, n, D, dtype=BF16) * 2
+    desc = ob.make_chunk_desc(Q, n_kv_heads=Hkv, causal=causal)
+    acc = torch.rand(1, Hkv, cache.cap, device="cuda")
+    before = host(acc)
+    with np.errstate(invalid="ignore"):
+        pool = cache.oracle()
+        O, lse = ob.omni_paged_attn(desc, Q, cache.pool, ints(ends), ints([n]), acc_in=acc, acc_out=acc)
+        wO, wl, ww, pv, qk = po.attend(host(Q), pool, np.array(ends), [n], causal, float(np.float32(desc.softmax_scale)))
+    _, el, ew = attend_bars(Q, pool, F32, 0, wO, wl, pv, qk, ww, before, H // Hkv, n)
+    dead = np.isneginf(wl)
+    assert np.array_equal(np.isneginf(host(lse)), dead)
+    within(host(lse)[~dead], wl[~dead], el[~dead], "lse")
+    for g in range(Hkv):
+        within(host(acc)[0, g, :ends[0][g]], (before + ww)[0, g, :ends[0][g]], ew[0, g, :ends[0][g]], "weights")
 
 
 # ------------------------------------------------------------------ eviction
