@@ -967,11 +967,18 @@ def _scratch(ws: Workspace | None, call_id: int, desc, param: int, dev):
     return torch.empty(workspace_bytes(call_id, desc, param), dtype=torch.uint8, device=dev)
 
 
+def _pool_tensors(pool: PagePool):
+    """Kpool, Vpool and page_table of a pool that make_page_pool made."""
+    if not hasattr(pool, "_keep"):
+        raise ValueError("the paged calls check the pool's tensors: make it with make_page_pool")
+    return pool._keep
+
+
 def _pool_of(pool: PagePool, dtype, head_dim: int, dev):
     """(batch, n_kv_heads, rows_cap) of a pool whose tensors fit the call."""
     facts = getattr(pool, "_facts", None)
     if facts is None:                             # of the tensors the pool was made of: they do not change
-        K, V, table = pool._keep
+        K, V, table = _pool_tensors(pool)
         if table.dim() != 3:
             raise ValueError("page_table must be [batch, n_kv_heads, pages_cap]")
         if V.dtype != K.dtype or V.device != K.device or table.device != K.device:
@@ -1034,6 +1041,8 @@ def omni_paged_append(desc: ChunkDesc, rope: RopeDesc | None, Q, K, V, pool: Pag
     _want_rows("K", K, dt, (B, Hkv, n, D), ks, dev)
     _want_rows("V", V, dt, (B, Hkv, n, D), ks, dev)
     if rope is not None:
+        if Q is None:
+            raise ValueError("rope turns the chunk's Q, too: give it")
         qs = (*desc.q_stride, 1)
         _want_rows("Q", Q, dt, (B, desc.n_q_heads, n, D), qs, dev)
         if Qout is None:
@@ -1096,7 +1105,7 @@ def omni_paged_evict(pool: PagePool, budget: int, n_sink: int, n_recent: int, se
     """Keep the `budget` rows of every pair that collected most attention weight (and those spared by their position), the rest
     of the pages free: (row_cnt, row_pos_out, acc_out).  Outputs that are not given are new tensors; pass row_pos and acc
     themselves to work in place."""
-    K, _, table = pool._keep
+    K = _pool_tensors(pool)[0]
     dev = K.device
     B, Hkv, cap = _pool_of(pool, K.dtype, K.shape[-1], dev)
     _want("seq_len", seq_len, torch.int32, (B,), dev)
