@@ -917,6 +917,7 @@ def omni_dense_decode(desc: DecodeDesc, q, Kcache, Vcache, ctx_len, O=None, ws: 
 #
 # These calls run on the current stream of their tensors' device.  Without a workspace of the caller's they take their
 # scratch from torch's allocator, call by call: calls on two streams, and two captured graphs, then never share any.
+# A Workspace is for one stream at a time, and is replaced where a call needs a larger one: a captured graph wants one of its own.
 
 _DTYPES = {OMNI_BF16: torch.bfloat16, OMNI_F32: torch.float32}
 
@@ -962,9 +963,12 @@ def _like(t: torch.Tensor, strides) -> torch.Tensor:
 
 
 def _scratch(ws: Workspace | None, call_id: int, desc, param: int, dev):
-    if ws is not None:
-        return ws.get(call_id, desc, param)
-    return torch.empty(workspace_bytes(call_id, desc, param), dtype=torch.uint8, device=dev)
+    if ws is None:
+        return torch.empty(workspace_bytes(call_id, desc, param), dtype=torch.uint8, device=dev)
+    buf = ws.get(call_id, desc, param)
+    if buf.device != dev:
+        raise ValueError(f"the workspace is on {buf.device}, the tensors are on {dev}")
+    return buf
 
 
 def _pool_tensors(pool: PagePool):
@@ -1125,7 +1129,7 @@ def omni_paged_evict(pool: PagePool, budget: int, n_sink: int, n_recent: int, se
     else:
         _want("acc_out", acc_out, torch.float32, (B, Hkv, cap), dev)
     d = _pairs_desc(pool)
-    buf = torch.empty(d._scratch, dtype=torch.uint8, device=dev) if ws is None else ws.get(CALL_PAGED_EVICT, d, cap)
+    buf = torch.empty(d._scratch, dtype=torch.uint8, device=dev) if ws is None else _scratch(ws, CALL_PAGED_EVICT, d, cap, dev)
     _run_on(dev, load_library().omni_paged_evict, C.byref(d), C.byref(pool), budget, n_sink, n_recent, seq_len.data_ptr(),
             row_end.data_ptr(), row_pos.data_ptr(), acc.data_ptr(), row_cnt.data_ptr(), row_pos_out.data_ptr(),
             acc_out.data_ptr(), buf.data_ptr(), buf.numel())

@@ -32,3 +32,12 @@ def test_a_pool_has_to_know_its_tensors(call):
                 lambda: ob.omni_paged_evict(bare, 4, 0, 0, cnt, ends, rows, rows.float())):
         with pytest.raises(ValueError, match="make_page_pool"):
             run()
+
+
+def test_scratch_on_another_device_is_refused(call):
+    Q, K, pool, desc, cnt, ends, rows = call
+    far = ob.Workspace("meta")
+    for run in (lambda: ob.omni_paged_attn(desc, Q, pool, ends, cnt, ws=far),
+                lambda: ob.omni_paged_evict(pool, 4, 0, 0, cnt, ends, rows, rows.float(), ws=far)):
+        with pytest.raises(ValueError, match="workspace"):
+            run()
