@@ -273,3 +273,13 @@ def test_eviction_below_a_border_stays_inside_its_scratch(pages):
                             row_pos_out=outs[0][:-256].view(1, 2, n), acc_out=outs[1][:-256].view(1, 2, n))
         ws.check()
         assert all((x[-256:] == -7).all() for x in outs)
+
+
+# ------------------------------------------------------------------ the binding
+
+def test_the_short_ways_to_stream_and_device_are_the_public_ones():
+    side = torch.cuda.Stream()
+    for stream in (torch.cuda.current_stream(), side):
+        with torch.cuda.stream(stream):
+            assert ob._raw_stream(0) == torch.cuda.current_stream().cuda_stream == stream.cuda_stream
+            assert ob._current_device() == torch.cuda.current_device()
