@@ -30,7 +30,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // A wavefront takes 32 cache rows per trip, K and V straight from the pages into a ring of two LDS stages of its own: while one is
 // worked on the other is on its way, 64 to 128 KB per CU in flight, and no barrier in the loop.  (Loads through registers, three
 // workgroups a CU, kept less in flight: 131k rows of eight sequences and four KV heads of 128 elements, a token each, took 567 us
-// with the weights, 415 now; 338 without them, 6.35 TB/s where a copy, which also writes, reaches 5.1.)  An instruction takes 1024
+// with the weights, 416 now; 327 without them, 6.5 TB/s where a copy, which also writes, reaches 5.1.)  An instruction takes 1024
 // bytes, whole rows of one page; the pieces of a row change places as in the tile kernel below.  Blocks with pages that are not there
 // go through registers.
 constexpr int kStreamWaves = 4, kStreamThreads = kStreamWaves * 64, kStreamRows = 32;
